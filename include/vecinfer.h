@@ -403,6 +403,169 @@ int vecinfer_export_value_codes(const vecinfer_cfg *cfg, const uint8_t *v_idx_ti
  */
 int vecinfer_read_probe(const void *src, size_t bytes, uint32_t *sink, void *stream);
 
+/*
+ * ---- Rotary positions and the full-precision paged cache ----------------------------------------
+ *
+ * Layers, sequences or recent tokens that are not quantized live in a paged cache: a pool of pages of
+ * page_size tokens, and per sequence a row of page numbers.  Its keys, and those that go to
+ * vecinfer_encode_keys, carry their positions.  The calls below turn queries and keys, write new
+ * tokens to their pages, attend to them, and cut a cache down to the tokens that matter.
+ *
+ * Elements are fp16 or bf16 (VECINFER_F16, VECINFER_BF16).  Strides are in elements, from one index of
+ * an axis to the next, not negative, multiples of 8 (rows are then read 16 bytes at a time) and below
+ * 2^30 for pages; the D channels of a row are adjacent.  Data pointers are 16-byte aligned.
+ */
+enum { VECINFER_F16 = 0, VECINFER_BF16 = 1 };
+
+/* How the frequencies f_i = base^(-2 i / R), i < R / 2, are scaled for contexts longer than the original. */
+enum {
+    VECINFER_ROTARY_PLAIN = 0,   /* not at all                                                          */
+    VECINFER_ROTARY_LINEAR = 1,  /* f_i / factor                                                        */
+    VECINFER_ROTARY_BASE = 2,    /* base * factor^(R / (R - 2)) in place of base                        */
+    VECINFER_ROTARY_PARTS = 3    /* by the turns r_i = orig_len f_i / (2 pi) that pair i makes in the original
+                                    context: g f_i + (1 - g) f_i / factor with
+                                    g = clamp((r_i - low_turns) / (high_turns - low_turns), 0, 1)       */
+};
+
+typedef struct vecinfer_rotary_cfg {
+    int32_t head_dim;      /* D: 64 or 128                                                              */
+    int32_t rot_dim;       /* R: the first R channels are turned, the others copied; multiple of 16, 16 .. D */
+    int32_t interleaved;   /* pairs of channels: 0 = (i, i + R / 2), 1 = (2 i, 2 i + 1)                  */
+    int32_t scaling;       /* VECINFER_ROTARY_*                                                         */
+    double base;           /* > 0                                                                       */
+    double factor;         /* > 0; scaling other than PLAIN                                             */
+    double low_turns, high_turns;   /* PARTS: low < high                                                */
+    int64_t orig_len;      /* PARTS: tokens of the original context, >= 1                               */
+    double magnitude;      /* m: factor of cosine and sine (1: lengths are kept), finite                */
+} vecinfer_rotary_cfg;
+
+/*
+ * Turns per position of the R / 2 pairs, as 64-bit fractions of a turn: table[i] = f_i / (2 pi) mod 1 in
+ * units of 2^-64, so that the angle of any position is exact to 2^-32 turns.  Made once per configuration.
+ *   freqs  fp64 [R / 2] on the device: frequencies (radians per position) in place of the formula's, or NULL
+ *   table  uint64 [R / 2] on the device, fully overwritten
+ * Errors: EINVAL for null or misaligned (8 bytes) pointers or values outside the ranges above;
+ * EUNSUPPORTED for head_dim or rot_dim.
+ */
+int vecinfer_rotary_table(const vecinfer_rotary_cfg *cfg, const double *freqs, uint64_t *table, void *stream);
+
+/*
+ * Rotary positions of B x H x T rows: every pair (x1, x2) of a row at position p becomes
+ *   m (x1 c - x2 s),  m (x1 s + x2 c),   c, s = cos, sin of p f_i,
+ * in fp32, rounded once.  inverse != 0: turned back by the same angle (s -> -s), still times m, which is
+ * the gradient with respect to x for a gradient given as x.
+ *   x, out     [B, H, T, D] by strides {b, h, t}; out may be x itself (same strides), else they may not overlap
+ *   positions  int32 [B, T] on the device, or NULL: token t has position pos0 + t
+ * Errors: EINVAL for null or misaligned pointers, B, H or T < 1, dtype or strides outside the ranges above,
+ * and a cfg as for vecinfer_rotary_table; EUNSUPPORTED for its head_dim or rot_dim, and B T >= 2^31.
+ */
+int vecinfer_rotary(const vecinfer_rotary_cfg *cfg, const uint64_t *table, int32_t dtype, const void *x,
+                    const int64_t x_strides[3], void *out, const int64_t out_strides[3], int32_t B, int32_t H,
+                    int64_t T, const int32_t *positions, int64_t pos0, int32_t inverse, void *stream);
+
+/*
+ * A pool of pages.  The rows of (page, KV head, slot) are at k + page k_strides[0] + head k_strides[1] +
+ * slot k_strides[2], and so for v; either order of heads and slots, or parts of a larger tensor, will do.
+ * Token t of a sequence is in slot t % page_size of page block_table[b, t / page_size].  A number outside
+ * 0 .. num_pages - 1 is a hole: nothing is read or written there, its tokens are not attended to and do
+ * not stay in an eviction.  Sequences may share pages that are only read; a page that is written belongs
+ * to one sequence.
+ */
+typedef struct vecinfer_pages {
+    void *k, *v;           /* device                                                                    */
+    int32_t dtype;         /* VECINFER_F16 or VECINFER_BF16                                             */
+    int32_t head_dim;      /* D: 64 or 128                                                              */
+    int32_t num_kv_heads;  /* H_kv                                                                      */
+    int32_t page_size;     /* tokens per page: a power of two, 8 .. 1024                                */
+    int64_t num_pages;     /* 1 .. 2^31 - 1                                                             */
+    int64_t k_strides[3], v_strides[3];   /* page, KV head, slot                                        */
+} vecinfer_pages;
+
+/*
+ * New tokens into the pages: keys turned by their positions, values as they are, and, if given, the
+ * queries of the same tokens turned into q_out, in one launch.  Token t < n_b of sequence b, n_b = new_lens[b]
+ * clamped to [0, T] or T, becomes token seq_lens[b] - n_b + t: seq_lens count the new tokens.  That is its
+ * position too, unless positions says another (a cache that tokens were evicted from is shorter than the
+ * text).  Tokens t >= n_b are padding: nothing of them is read for or written to the pages or q_out.  A
+ * token that comes to lie before 0, behind the table or in a hole is not written; its query is turned.
+ *   rot, table  NULL: keys are written as they are (q has to be NULL then)
+ *   k_new, v_new  [B, H_kv, T, D] by strides {b, h, t}        q, q_out  [B, H_q, T, D], or both NULL
+ *   block_table   int32 [B, max_pages]    seq_lens  int32 [B]    new_lens  int32 [B] or NULL
+ *   positions     int32 [B, T] or NULL
+ *   weights       fp32 [B, H_kv, w_cap] or NULL: the sums of vecinfer_paged_attention, set to 0 for the new
+ *                 tokens below w_cap
+ * Errors: EINVAL (null or misaligned pointers, sizes < 1, strides, q without rot or without q_out, pages or
+ * cfg outside their ranges, different head_dim), EUNSUPPORTED (head_dim, rot_dim, page_size; B T >= 2^31).
+ */
+int vecinfer_paged_append(const vecinfer_pages *pages, const vecinfer_rotary_cfg *rot, const uint64_t *table,
+                          const void *k_new, const int64_t k_strides[3], const void *v_new,
+                          const int64_t v_strides[3], const void *q, const int64_t q_strides[3], void *q_out,
+                          const int64_t q_out_strides[3], int32_t num_q_heads, const int32_t *block_table,
+                          int64_t max_pages, const int32_t *seq_lens, const int32_t *new_lens,
+                          const int32_t *positions, int32_t B, int64_t T, float *weights, int64_t w_cap,
+                          void *stream);
+
+/*
+ * Workspace of vecinfer_paged_attention for batch B, up to N tokens and num_splits splits (0 = as many as it
+ * takes by itself); weights != 0: with weights_out.  Host-only; 0 for invalid arguments.  As for the other
+ * decode calls, one with num_splits = 0 that is given less takes fewer splits, down to one.
+ */
+size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q_heads, int32_t B, int64_t N,
+                                      int32_t num_splits, int32_t weights);
+
+/*
+ * Attention of one new token per sequence over its pages (the new token among them: append first):
+ *   s_t = scale q . k_t  over t < len_b that are not in a hole;   o = softmax(s) v;   L = log sum_t exp(s_t)
+ * per (b, query head h), KV head h / G, G = H_q / H_kv in 1 .. 16.  Products and sums in fp32, one rounding of
+ * the output.  Without a token to attend to (or with scores of -inf alone) o = 0 and L = -inf.  What the rows
+ * behind a sequence's end hold is of no account, infinities and NaN included.
+ *   q          [B, H_q, D] by strides {b, h}             out  [B, H_q, D], contiguous, of the pages' type
+ *   seq_lens   int32 [B] or NULL: N tokens each; clamped to [0, N]
+ *   N          1 <= N <= max_pages page_size, N <= 2^30
+ *   num_splits 0 = auto, else 1 .. VECINFER_MAX_SPLITS
+ *   lse        fp32 [B, H_q] or NULL
+ *   weights_in, weights_out  fp32 [B, H_kv, w_cap], w_cap >= N, or both NULL: for t < len_b
+ *              weights_out[b, g, t] = weights_in[b, g, t] + sum over the G heads of softmax(s)_t
+ *              (holes: + 0).  weights_in may be weights_out, or NULL: 0.  Rows t >= len_b are left as they
+ *              were.  With weights a second launch follows.
+ *   workspace  as for vecinfer_decode_attention
+ * Errors: EINVAL (null or misaligned pointers, sizes, strides, scale not finite, w_cap < N, weights_in alone),
+ * EUNSUPPORTED (pages, G, B or H_kv above 65535, N > 2^30), EWORKSPACE, ELAUNCH.
+ */
+int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const int64_t q_strides[2],
+                             int32_t num_q_heads, const int32_t *block_table, int64_t max_pages,
+                             const int32_t *seq_lens, int32_t B, int64_t N, float scale, int32_t num_splits,
+                             void *workspace, size_t workspace_bytes, void *out, float *lse,
+                             const float *weights_in, float *weights_out, int64_t w_cap, void *stream);
+
+/*
+ * Eviction by accumulated attention weight.  Of the len_b tokens of sequence b each KV head keeps at most
+ * `keep`: the first `first` and the last `recent` of them, and of the others those of the largest weight, the
+ * lowest index first among equals (-0 equals 0; what is not a number comes below all numbers).  Kept tokens
+ * keep their order and become tokens 0, 1, .. of the sequence in the pages of dst_table, heads apart: other
+ * heads keep other tokens, all of them the same number of them, min(keep, tokens outside holes), which goes
+ * to dst_lens.  A token whose new page is a hole is not written.  The rows carry their positions with them;
+ * new tokens are then appended with `positions`.
+ *   weights      fp32 [B, H_kv, w_cap], w_cap >= N
+ *   src, dst     pools of one type, head_dim and H_kv (page sizes may differ); dst may be src, but the pages of
+ *                dst_table must not be pages that this call reads
+ *   N, seq_lens  as for vecinfer_paged_attention           dst_table  int32 [B, dst_max_pages]
+ *   keep         1 <= keep <= dst_max_pages dst->page_size, first + recent <= keep
+ *   dst_lens     int32 [B], not seq_lens
+ *   dst_weights  fp32 [B, H_kv, dst_w_cap], dst_w_cap >= keep, not weights, or NULL: the kept tokens' weights
+ *   kept         int32 [B, H_kv, keep] or NULL: their old indices, in order (rows from dst_lens on are left)
+ *   workspace    vecinfer_evict_workspace_bytes(H_kv, B, N, keep) bytes, 256-byte aligned
+ * Errors: EINVAL (null or misaligned pointers, sizes, pools that do not match, dst_lens = seq_lens,
+ * dst_weights = weights), EUNSUPPORTED (pages, B or H_kv above 65535, N > 2^30), EWORKSPACE, ELAUNCH.
+ */
+size_t vecinfer_evict_workspace_bytes(int32_t num_kv_heads, int32_t B, int64_t N, int64_t keep);
+int vecinfer_paged_evict(const vecinfer_pages *src, const float *weights, int64_t w_cap,
+                         const int32_t *block_table, int64_t max_pages, const int32_t *seq_lens, int32_t B,
+                         int64_t N, int64_t keep, int64_t first, int64_t recent, const vecinfer_pages *dst,
+                         const int32_t *dst_table, int64_t dst_max_pages, int32_t *dst_lens, float *dst_weights,
+                         int64_t dst_w_cap, int32_t *kept, void *workspace, size_t workspace_bytes,
+                         void *stream);
+
 /* Human-readable text for a return code (static storage). */
 const char *vecinfer_strerror(int code);
 

@@ -30,6 +30,8 @@ EXPORTS = [
     "vecinfer_kmeans_workspace_bytes", "vecinfer_kmeans_step", "vecinfer_kmeans_train",
     "vecinfer_index_row_bytes", "vecinfer_codebook_elems", "vecinfer_calibrate_lambda", "vecinfer_read_probe",
     "vecinfer_export_value_codes",
+    "vecinfer_rotary_table", "vecinfer_rotary", "vecinfer_paged_append", "vecinfer_paged_workspace_bytes",
+    "vecinfer_paged_attention", "vecinfer_evict_workspace_bytes", "vecinfer_paged_evict",
     "vecinfer_strerror", "vecinfer_version",
 ]
 
@@ -118,6 +120,70 @@ class Config:
         return self.head_dim // d * bits // 8
 
 
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+_TYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+class _RotaryCfg(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("head_dim", "rot_dim", "interleaved", "scaling")] +
+                [(n, C.c_double) for n in ("base", "factor", "low_turns", "high_turns")] +
+                [("orig_len", C.c_int64), ("magnitude", C.c_double)])
+
+
+class _Pages(C.Structure):
+    _fields_ = ([("k", C.c_void_p), ("v", C.c_void_p)] +
+                [(n, C.c_int32) for n in ("dtype", "head_dim", "num_kv_heads", "page_size")] +
+                [("num_pages", C.c_int64), ("k_strides", C.c_int64 * 3), ("v_strides", C.c_int64 * 3)])
+
+
+@dataclass(frozen=True)
+class Rotary:
+    """Mirror of ``vecinfer_rotary_cfg``."""
+    head_dim: int
+    rot_dim: int
+    interleaved: int = 0        # 0: pairs (i, i + R / 2), 1: pairs (2 i, 2 i + 1)
+    base: float = 10000.0
+    scaling: int = ROTARY_PLAIN
+    factor: float = 1.0
+    orig_len: int = 0
+    low_turns: float = 1.0
+    high_turns: float = 32.0
+    magnitude: float = 1.0
+
+    @_once
+    def _c(self) -> _RotaryCfg:
+        return _RotaryCfg(self.head_dim, self.rot_dim, self.interleaved, self.scaling, self.base, self.factor, self.low_turns,
+                          self.high_turns, self.orig_len, self.magnitude)
+
+    def __getstate__(self):
+        return {f: self.__dict__[f] for f in self.__dataclass_fields__}
+
+
+class Pages:
+    """A pool of pages for the paged calls: keys and values [num_pages, H_kv, page_size, D], fp16 or bf16 of any strides
+    with adjacent channels (``pool.transpose(1, 2)`` of a [num_pages, page_size, H_kv, D] tensor, say)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if not isinstance(k, torch.Tensor) or not isinstance(v, torch.Tensor) or not k.is_cuda or not v.is_cuda:
+            raise TypeError("pages: expected tensors on the GPU")
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _TYPES or k.device != v.device:
+            raise ValueError("pages: expected two fp16 or bf16 tensors [num_pages, H_kv, page_size, D] of one shape on one device")
+        self.k, self.v = k, v
+        self.num_pages, self.num_kv_heads, self.page_size, self.head_dim = k.shape
+        self._c = _Pages(k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], self.head_dim, self.num_kv_heads, self.page_size,
+                         self.num_pages, _steps(k, "k", True), _steps(v, "v", True))
+
+
+def _steps(t: torch.Tensor, name: str, written: bool):
+    """Strides of all axes but the last, whose elements have to be adjacent; an axis of one index has none."""
+    s = [st if n > 1 else 0 for n, st in zip(t.shape, t.stride())]
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last axis has to be contiguous")
+    if written and any(n > 1 and st == 0 for n, st in zip(t.shape, s)):
+        raise ValueError(f"{name}: is written, and has rows on top of each other")
+    return (C.c_int64 * (len(s) - 1))(*s[:-1])
+
+
 class VecInferError(RuntimeError):
     def __init__(self, code: int):
         self.code = code
@@ -176,6 +242,24 @@ def lib() -> C.CDLL:
         L.vecinfer_index_row_bytes.restype = sz
         L.vecinfer_codebook_elems.argtypes = [cfgp, i32]
         L.vecinfer_codebook_elems.restype = sz
+        rotp, pagesp, i64p = C.POINTER(_RotaryCfg), C.POINTER(_Pages), C.POINTER(i64)
+        L.vecinfer_rotary_table.argtypes = [rotp, vp, vp, vp]
+        L.vecinfer_rotary_table.restype = C.c_int
+        L.vecinfer_rotary.argtypes = [rotp, vp, i32, vp, i64p, vp, i64p, i32, i32, i64, vp, i64, i32, vp]
+        L.vecinfer_rotary.restype = C.c_int
+        L.vecinfer_paged_append.argtypes = [pagesp, rotp, vp, vp, i64p, vp, i64p, vp, i64p, vp, i64p, i32, vp, i64, vp, vp, vp,
+                                            i32, i64, vp, i64, vp]
+        L.vecinfer_paged_append.restype = C.c_int
+        L.vecinfer_paged_workspace_bytes.argtypes = [pagesp, i32, i32, i64, i32, i32]
+        L.vecinfer_paged_workspace_bytes.restype = sz
+        L.vecinfer_paged_attention.argtypes = [pagesp, vp, i64p, i32, vp, i64, vp, i32, i64, C.c_float, i32, vp, sz, vp, vp, vp,
+                                               vp, i64, vp]
+        L.vecinfer_paged_attention.restype = C.c_int
+        L.vecinfer_evict_workspace_bytes.argtypes = [i32, i32, i64, i64]
+        L.vecinfer_evict_workspace_bytes.restype = sz
+        L.vecinfer_paged_evict.argtypes = [pagesp, vp, i64, vp, i64, vp, i32, i64, i64, i64, i64, pagesp, vp, i64, vp, vp, i64,
+                                           vp, vp, sz, vp]
+        L.vecinfer_paged_evict.restype = C.c_int
         L.vecinfer_strerror.argtypes = [C.c_int]
         L.vecinfer_strerror.restype = C.c_char_p
         L.vecinfer_version.restype = C.c_int
@@ -492,3 +576,159 @@ def vecinfer_kmeans_train(cfg: Config, x_f16, lam, cb, codes, workspace, counts=
         None if iters_run is None else _dev(iters_run, torch.int32, (1,), "iters_run"),
         None if errors is None else _dev(errors, torch.float64, (max_iters,), "errors"),
         workspace.data_ptr(), workspace.numel(), _stream(stream)))
+
+
+def _here(t: torch.Tensor, name: str) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a tensor on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t
+
+
+def _rows(t: torch.Tensor, dtype, shape, name: str, written: bool = False):
+    """Pointer and strides of a tensor of any strides with adjacent channels."""
+    if _here(t, name).dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr(), _steps(t, name, written)
+
+
+def _flat(t: torch.Tensor | None, dtype, shape, name: str) -> int | None:
+    """Pointer of a contiguous tensor on the current device, or None."""
+    return None if t is None else _dev(_here(t, name), dtype, shape, name)
+
+
+def _workspace(t: torch.Tensor) -> tuple:
+    if not _here(t, "workspace").is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _pool(p: Pages, name: str) -> "C._Pointer":
+    if not isinstance(p, Pages):
+        raise TypeError(f"{name}: expected Pages")
+    _here(p.k, name)
+    return C.byref(p._c)
+
+
+def vecinfer_rotary_table(rot: Rotary, table, freqs=None, stream=None) -> None:
+    """Turns per position of every pair into table, int64 [R / 2] (64-bit fractions of a turn); freqs: float64 [R / 2]
+    radians per position in place of the configuration's formula."""
+    n = rot.rot_dim // 2
+    _check(lib().vecinfer_rotary_table(C.byref(rot._c), _flat(freqs, torch.float64, (n,), "freqs"),
+                                       _flat(table, torch.int64, (n,), "table"), _stream(stream)))
+
+
+def new_rotary_table(rot: Rotary, freqs=None, device="cuda") -> torch.Tensor:
+    table = torch.empty(max(rot.rot_dim // 2, 0), dtype=torch.int64, device=device)
+    vecinfer_rotary_table(rot, table, freqs)
+    return table
+
+
+def vecinfer_rotary(rot: Rotary, table, x, out, positions=None, pos0: int = 0, inverse: int = 0, stream=None) -> None:
+    """Turn x [B, H, T, D] (fp16 or bf16, any strides) into out by its positions: int32 [B, T], or pos0 + t.  out may be
+    x.  inverse: turn back, which takes the gradient of out to that of x."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 4 or x.dtype not in _TYPES:
+        raise ValueError("x: expected fp16 or bf16 [B, H, T, D]")
+    B, H, T, D = x.shape
+    px, sx = _rows(x, x.dtype, (B, H, T, rot.head_dim), "x")
+    po, so = _rows(out, x.dtype, (B, H, T, rot.head_dim), "out", True)
+    _check(lib().vecinfer_rotary(C.byref(rot._c), _flat(table, torch.int64, (rot.rot_dim // 2,), "table"), _TYPES[x.dtype],
+                                 px, sx, po, so, B, H, T, _flat(positions, torch.int32, (B, T), "positions"), pos0,
+                                 1 if inverse else 0, _stream(stream)))
+
+
+def vecinfer_paged_append(pages: Pages, k_new, v_new, block_table, seq_lens, new_lens=None, rot: Rotary | None = None,
+                          table=None, positions=None, q=None, q_out=None, weights=None, stream=None) -> None:
+    """Write T new tokens per sequence, k_new and v_new [B, Hkv, T, D], to their pages (block_table int32 [B, max_pages]),
+    keys turned by `rot`; turn the queries q [B, Hq, T, D] into q_out.  seq_lens [B] count the new tokens, of which
+    sequence b has new_lens[b] (or T)."""
+    pool, dtype = _pool(pages, "pages"), pages.k.dtype
+    B, Hkv, T, D = k_new.shape
+    shape = (B, pages.num_kv_heads, T, pages.head_dim)
+    pk, sk = _rows(k_new, dtype, shape, "k_new")
+    pv, sv = _rows(v_new, dtype, shape, "v_new")
+    pq = sq = po = so = None
+    Hq = 0
+    if q is not None:
+        Hq = q.shape[1]
+        pq, sq = _rows(q, dtype, (B, Hq, T, pages.head_dim), "q")
+    if q_out is not None:
+        po, so = _rows(q_out, dtype, (B, Hq, T, pages.head_dim), "q_out", True)
+    w_cap = 0 if weights is None else weights.shape[-1]
+    _check(lib().vecinfer_paged_append(
+        pool, None if rot is None else C.byref(rot._c),
+        None if rot is None else _flat(table, torch.int64, (rot.rot_dim // 2,), "table"), pk, sk, pv, sv, pq, sq, po, so, Hq,
+        _flat(block_table, torch.int32, (B, block_table.shape[-1]), "block_table"), block_table.shape[-1],
+        _flat(seq_lens, torch.int32, (B,), "seq_lens"), _flat(new_lens, torch.int32, (B,), "new_lens"),
+        _flat(positions, torch.int32, (B, T), "positions"), B, T,
+        _flat(weights, torch.float32, (B, pages.num_kv_heads, w_cap), "weights"), w_cap, _stream(stream)))
+
+
+def vecinfer_paged_workspace_bytes(pages: Pages, num_q_heads: int, B: int, N: int, num_splits: int = 0, weights: int = 0) -> int:
+    return int(lib().vecinfer_paged_workspace_bytes(_pool(pages, "pages"), num_q_heads, B, N, num_splits, 1 if weights else 0))
+
+
+def new_paged_workspace(pages: Pages, num_q_heads: int, B: int, N: int, num_splits: int = 0, weights: int = 0) -> torch.Tensor:
+    """Allocate (with torch) a workspace for vecinfer_paged_attention."""
+    nbytes = vecinfer_paged_workspace_bytes(pages, num_q_heads, B, N, num_splits, weights)
+    if nbytes == 0:
+        raise VecInferError(EUNSUPPORTED)
+    return torch.empty(nbytes, dtype=torch.uint8, device=pages.k.device)
+
+
+def vecinfer_paged_attention(pages: Pages, q, block_table, workspace, out, lse=None, seq_lens=None, N: int | None = None,
+                             scale: float | None = None, num_splits: int = 0, weights_in=None, weights_out=None,
+                             stream=None) -> None:
+    """Attention of one new token per sequence, q [B, Hq, D] (any strides), over its pages; writes out [B, Hq, D] (and lse
+    [B, Hq]).  scale: 1 / sqrt(D) unless given.  weights_out [B, Hkv, w_cap] = weights_in (or 0) + the attention weights
+    of the step, summed over the heads of a KV head; weights_in may be weights_out."""
+    pool = _pool(pages, "pages")
+    B, Hq, D = q.shape
+    dtype = pages.k.dtype
+    pq, sq = _rows(q, dtype, (B, Hq, pages.head_dim), "q")
+    max_pages = block_table.shape[-1]
+    N = max_pages * pages.page_size if N is None else N
+    w_cap = 0 if weights_out is None else weights_out.shape[-1]
+    if weights_out is None and weights_in is not None:
+        raise VecInferError(EINVAL)
+    wp, wb = _workspace(workspace)
+    _check(lib().vecinfer_paged_attention(
+        pool, pq, sq, Hq, _flat(block_table, torch.int32, (B, max_pages), "block_table"), max_pages,
+        _flat(seq_lens, torch.int32, (B,), "seq_lens"), B, N, pages.head_dim ** -0.5 if scale is None else scale, num_splits,
+        wp, wb, _flat(out, dtype, (B, Hq, pages.head_dim), "out"), _flat(lse, torch.float32, (B, Hq), "lse"),
+        _flat(weights_in, torch.float32, (B, pages.num_kv_heads, w_cap), "weights_in"),
+        _flat(weights_out, torch.float32, (B, pages.num_kv_heads, w_cap), "weights_out"), w_cap, _stream(stream)))
+
+
+def vecinfer_evict_workspace_bytes(num_kv_heads: int, B: int, N: int, keep: int) -> int:
+    return int(lib().vecinfer_evict_workspace_bytes(num_kv_heads, B, N, keep))
+
+
+def new_evict_workspace(pages: Pages, B: int, N: int, keep: int) -> torch.Tensor:
+    """Allocate (with torch) a workspace for vecinfer_paged_evict."""
+    nbytes = vecinfer_evict_workspace_bytes(pages.num_kv_heads, B, N, keep)
+    if nbytes == 0:
+        raise VecInferError(EUNSUPPORTED)
+    return torch.empty(nbytes, dtype=torch.uint8, device=pages.k.device)
+
+
+def vecinfer_paged_evict(pages: Pages, weights, block_table, dst_pages: Pages, dst_table, dst_lens, workspace, keep: int,
+                         first: int = 0, recent: int = 0, seq_lens=None, N: int | None = None, dst_weights=None, kept=None,
+                         stream=None) -> None:
+    """Keep, per sequence and KV head, the first `first` and last `recent` tokens and those of the largest weights
+    [B, Hkv, w_cap], `keep` in all, in order, in the pages of dst_table [B, dst_max_pages] (of `dst_pages`, which may be
+    `pages`; not pages that are read).  Writes dst_lens [B] and, if given, dst_weights [B, Hkv, dst_w_cap] and the kept
+    tokens' old indices, kept [B, Hkv, keep].  N: as many tokens as weights has, at most, unless given."""
+    src, dst = _pool(pages, "pages"), _pool(dst_pages, "dst_pages")
+    B, max_pages = block_table.shape
+    Hkv, w_cap = pages.num_kv_heads, weights.shape[-1]
+    dst_w_cap = 0 if dst_weights is None else dst_weights.shape[-1]
+    N = min(w_cap, max_pages * pages.page_size) if N is None else N
+    wp, wb = _workspace(workspace)
+    _check(lib().vecinfer_paged_evict(
+        src, _flat(weights, torch.float32, (B, Hkv, w_cap), "weights"), w_cap,
+        _flat(block_table, torch.int32, (B, max_pages), "block_table"), max_pages, _flat(seq_lens, torch.int32, (B,), "seq_lens"),
+        B, N, keep, first, recent, dst, _flat(dst_table, torch.int32, (B, dst_table.shape[-1]), "dst_table"), dst_table.shape[-1],
+        _flat(dst_lens, torch.int32, (B,), "dst_lens"), _flat(dst_weights, torch.float32, (B, Hkv, dst_w_cap), "dst_weights"),
+        dst_w_cap, _flat(kept, torch.int32, (B, Hkv, keep), "kept"), wp, wb, _stream(stream)))

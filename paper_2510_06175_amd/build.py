@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libvecinfer.so")
 # the hot calls' argument checks, see csrc/fastcall.cpp; named after the interpreter it is built for, so that no other loads it
 FASTCALL = os.path.join(HERE, "_fastcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["api.hip", "merge.hip", "encode.hip", "calibrate.hip", "probe.hip", "decode_lut.hip", "decode_roles.hip"]
+SOURCES = ["api.hip", "merge.hip", "encode.hip", "calibrate.hip", "probe.hip", "decode_lut.hip", "decode_roles.hip",
+           "paged_api.hip", "rotary.hip", "paged_attention.hip", "evict.hip"]
 # the matrix-core attention kernels, compiled once for the calls without a residual window and once for those with one
 MFMA_SOURCES = ["decode_mfma.hip", "decode_mfma_wide.hip", "decode_mfma_wide64.hip", "decode_mfma_tiled.hip"]
 

@@ -58,6 +58,18 @@ int num_cus()
     return cached;
 }
 
+// A launch's own number (split_merge.h): 48 bits, not 0.  Counted from a start of the process's own, so that a
+// word that something else left behind in memory is no more likely to carry it than any other number.
+unsigned long long next_nonce()
+{
+    static std::atomic<unsigned long long> count{
+        (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull};
+    unsigned long long n;
+    do n = count.fetch_add(1, std::memory_order_relaxed) & 0xffffffffffffull;
+    while (n == 0);
+    return n;
+}
+
 } // namespace vecinfer
 
 namespace {
@@ -230,18 +242,6 @@ WorkspaceLayout ws_layout(const vecinfer_cfg *c, int32_t B, int32_t S)
     off += up(sizeof(float) * (size_t)B * c->num_kv_heads * c->head_dim);
     w.total = off;
     return w;
-}
-
-// A launch's own number (split_merge.h): 48 bits, not 0.  Counted from a start of the process's own, so that a
-// word that something else left behind in memory is no more likely to carry it than any other number.
-unsigned long long next_nonce()
-{
-    static std::atomic<unsigned long long> count{
-        (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull};
-    unsigned long long n;
-    do n = count.fetch_add(1, std::memory_order_relaxed) & 0xffffffffffffull;
-    while (n == 0);
-    return n;
 }
 
 // Validates one encode request and fills the kernel arguments; VECINFER_OK or an error code.

@@ -186,6 +186,7 @@ __device__ __forceinline__ void finish_split(const DecodeParams &p, int b, int g
 constexpr int kMaxResidual = 128;                  // rows of the residual window (the paper's setting)
 
 int num_cus();   // compute units of the chip (queried once per process; sizes grids only)
+unsigned long long next_nonce();   // a launch's own number (split_merge.h)
 
 // launchers (one translation unit each)
 int launch_merge(const DecodeParams &p, hipStream_t stream);   // splits (+ residual window) -> out, lse

@@ -1,0 +1,102 @@
+// Shared definitions of the operators around the full-precision paged cache: rotary positions, append, attention,
+// eviction.
+#pragma once
+#include "common.h"
+
+namespace vecinfer {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+// A paged cache.  Row (page, KV head h, slot) of the keys is the D elements at
+//   k + page * k_page + h * k_head + slot * k_slot      (bytes; every step below 2^31, a multiple of 16)
+// and the page of token t of sequence b is block_table[b, t / page_size].  A page number outside
+// 0 .. num_pages - 1 is a hole: its tokens are not attended to, kept or written.
+struct PageSet {
+    char *k, *v;
+    unsigned k_page, k_head, k_slot, v_page, v_head, v_slot;
+    unsigned num_pages;
+    int shift;                   // log2 of the page size
+};
+
+struct RowSet {                  // rows [B, H, T, D] in memory, steps in bytes
+    const char *in;
+    char *out;
+    long long in_b, in_h, in_t, out_b, out_h, out_t;
+    int heads;
+};
+
+struct RotaryParams {
+    RowSet x;                    // the tensor to turn (append: the queries; heads = 0: none)
+    RowSet k, v;                 // append only: new keys and values (out_* unused)
+    PageSet pages;
+    const int32_t *block_table;  // [B, max_pages]
+    long long max_pages;
+    const int32_t *seq_lens;     // [B] lengths with the new tokens
+    const int32_t *new_lens;     // [B] or nullptr: T
+    const uint64_t *table;       // [R / 2] turns per position, in units of 2^-64
+    const int32_t *positions;    // [B, T] or nullptr
+    long long pos0;              // position of token 0 (not append)
+    float *weights;              // [B, Hkv, w_cap] or nullptr: cleared for the new tokens
+    long long w_cap;
+    int B, T, R, interleaved;
+    float sign, magnitude;
+};
+
+struct PagedParams {
+    PageSet pages;
+    const char *q;               // rows (b, h) at q + b * q_b + h * q_h bytes
+    long long q_b, q_h;
+    const int32_t *block_table;  // [B, max_pages]
+    long long max_pages;
+    const int32_t *seq_lens;     // [B] or nullptr: N
+    int B, Hq, Hkv, G, N, S;
+    float scale2;                // softmax scale * log2(e)
+    float *part_o;               // [B, Hkv, S, G, D]  partials, as in DecodeParams
+    float *part_m, *part_l;      // [B, Hkv, S, G]
+    unsigned long long *words;   // [B, Hkv] arrival words (split_merge.h)
+    unsigned long long nonce;
+    void *out;                   // [B, Hq, D]
+    float *lse;                  // [B, Hq] or nullptr
+    // sums of attention weight; scores == nullptr: none
+    float *scores;               // [B, Hq, n_pad] scores in log2 units
+    float *lse2;                 // [B, Hq] log2 of the sum of exp2 of the scores
+    long long n_pad;
+    const float *w_in;           // [B, Hkv, w_cap] or nullptr: 0
+    float *w_out;                // [B, Hkv, w_cap]
+    long long w_cap;
+};
+
+struct EvictParams {
+    PageSet src, dst;
+    const float *w;              // [B, Hkv, w_cap]
+    long long w_cap;
+    const int32_t *block_table, *dst_table;
+    long long max_pages, dst_max_pages;
+    const int32_t *seq_lens;     // [B] or nullptr: N
+    int B, Hkv, D, N, keep, first, recent;
+    int32_t *dst_lens;           // [B]
+    float *dst_w;                // [B, Hkv, dst_w_cap] or nullptr
+    long long dst_w_cap;
+    int32_t *kept;               // [B, Hkv, keep] or nullptr
+    int32_t *ids;                // [B, Hkv, min(keep, N)] in the workspace: the kept tokens, for the move
+};
+
+__device__ __forceinline__ int clamped_len(const int32_t *lens, int b, int N)
+{
+    if (!lens) return N;
+    const int v = lens[b];
+    return v < 0 ? 0 : (v > N ? N : v);
+}
+
+// log2 of the sum, and the sum itself, go to natural units in one place
+__device__ __forceinline__ float natural(float log2_units) { return log2_units * kLn2; }
+
+int launch_rotary_table(const double *freqs, double base, int scaling, double factor, double low, double high,
+                        double orig_len, int R, uint64_t *table, hipStream_t stream);
+int launch_rotary(const RotaryParams &p, int bf16, int D, bool append, hipStream_t stream);
+int launch_paged_attention(const PagedParams &p, int bf16, int D, hipStream_t stream);
+int launch_paged_weights(const PagedParams &p, hipStream_t stream);
+int launch_evict(const EvictParams &p, hipStream_t stream);
+
+} // namespace vecinfer

@@ -1,0 +1,384 @@
+// Decode attention over a full-precision paged cache, one new token per sequence.
+//
+//   s_t = scale q . k_t,   o = sum_t p_t v_t,   p = softmax(s),   L = log sum_t exp(s_t)
+//
+// One workgroup per (split, KV head, sequence), all G query heads of the KV head in it, so that a key or value row is
+// read once.  Its wavefronts are independent: each takes every NW-th tile of 32 tokens of the split, keeps the running
+// maximum and sum of its own tiles, and joins the others at the end, through LDS.
+//
+// A tile never leaves registers.  Both products are 16x16x32 matrix instructions with the query heads in the 16
+// columns, and the tokens are dealt to the rows so that one's result is the other's operand:
+//   scores   A = keys: row m of sub-tile u is token 8 (m / 4) + 4 u + m % 4; B = queries.  Lane (kg = l / 16, c = l % 16)
+//            gets the scores of head c, tokens 8 kg + 4 u + r;
+//   output   A = values, transposed; B = the probabilities: lane (kg, c) holds head c, tokens 8 kg .. 8 kg + 7 - which
+//            are those it has.  Of the values lane (kg, c) loads D / 16 channels from channel c D / 16 of tokens
+//            8 kg .. + 7, whole rows per 16 lanes, and turns the block within its own registers.  Row m of the i-th
+//            product is then channel m D / 16 + i.
+// What bounds it is memory: 4 D bytes per token against 32 D G / 16 matrix operations, of which the chip has 50 times
+// as many per byte as are needed.  So the idle columns (G < 16) cost nothing, nor do the probabilities as two parts
+// (high and low), which leave no error of their own next to the output's rounding.  The one with 16 bits alone would
+// add as much again.
+#include "mfma_helpers.h"
+#include "paged.h"
+#include "split_merge.h"
+
+namespace vecinfer {
+
+namespace {
+
+constexpr int kTokens = 32;                               // tokens of a tile
+
+template <typename E> struct Vec;
+template <> struct Vec<f16> {
+    typedef f16 v8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ floatx4 mfma(v8 a, v8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    // Probabilities are held times 2^15: fp16 then has them in full down to 2^-29 of the largest.
+    static constexpr float kLift = 15.f;
+};
+template <> struct Vec<bf16> {
+    typedef bf16 v8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ floatx4 mfma(v8 a, v8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static constexpr float kLift = 0.f;
+};
+
+// sum over the four 16-lane rows of the wavefront
+__device__ __forceinline__ float rows_sum(float x)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    auto s16 = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const float m = __builtin_bit_cast(float, (unsigned)s16[0]) + __builtin_bit_cast(float, (unsigned)s16[1]);
+    const unsigned w = __builtin_bit_cast(unsigned, m);
+    auto s32 = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return __builtin_bit_cast(float, (unsigned)s32[0]) + __builtin_bit_cast(float, (unsigned)s32[1]);
+}
+
+template <typename E>
+__device__ __forceinline__ typename Vec<E>::v8 as_vec(unsigned a, unsigned b, unsigned c, unsigned d)
+{
+    const uintx4 u = {a, b, c, d};
+    return __builtin_bit_cast(typename Vec<E>::v8, u);
+}
+
+// Called by all threads of a workgroup whose partials are stored: the last of the S workgroups of this (sequence, KV
+// head) writes the output rows (split_merge.h).
+template <typename E, int D, int KG, int NW>
+__device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, size_t bg, size_t row0)
+{
+    constexpr int kBlock = NW * 64, kBatch = 16;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), S = p.S, G = p.G;
+    arrival_t *const word = p.words + bg;
+    unsigned *const flag = reinterpret_cast<unsigned *>(lds);
+    float *const wt_s = lds + 4, *const den_s = wt_s + KG * kMergeSplits;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's stores are acknowledged
+    __syncthreads();
+    if (t == 0) {
+        const arrival_t before = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = (int)(before & 0xffffu) == S - 1;
+    }
+    __syncthreads();
+    if (*flag == 0u) return;                              // (the same for the whole workgroup)
+    if (t == 0) __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int h = wave; h < G; h += NW) {
+        const float *const pm = p.part_m + bg * S * G + h, *const pl = p.part_l + bg * S * G + h;
+        float m[kMergeSplits / 64], l[kMergeSplits / 64], M = -INFINITY, den = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMergeSplits / 64; ++i) {
+            const int s = lane + 64 * i;
+            m[i] = s < S ? shared_load(pm + (size_t)s * G) : -INFINITY;
+            l[i] = s < S ? shared_load(pl + (size_t)s * G) : 0.f;
+            M = fmaxf(M, m[i]);
+        }
+        M = wave_max(M);
+        const float at = M > -INFINITY ? M : 0.f;         // nothing to attend to: all weights 0
+#pragma unroll
+        for (int i = 0; i < kMergeSplits / 64; ++i) {
+            const float w = __builtin_amdgcn_exp2f(m[i] - at);
+            wt_s[h * kMergeSplits + lane + 64 * i] = w;
+            den = fmaf(w, l[i], den);
+        }
+        den = wave_sum(den);
+        if (lane == 0) {
+            const float total = den == 0.f ? -INFINITY : M + log2f(den);
+            den_s[h] = den;
+            if (p.lse) p.lse[row0 + h] = natural(total);
+            if (p.lse2) p.lse2[row0 + h] = total;
+        }
+    }
+    __syncthreads();
+    const float *const po = p.part_o + bg * S * G * D;
+    E *const out = static_cast<E *>(p.out) + row0 * D;
+    for (int e = t; e < G * D; e += kBlock) {
+        const int h = e / D;
+        float acc = 0.f;
+        for (int s0 = 0; s0 < S; s0 += kBatch) {
+            float v[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) v[j] = shared_load(po + (size_t)(s0 + j < S ? s0 + j : S - 1) * G * D + e);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)              // (behind the last split the weights are 0: m = -inf)
+                if (s0 + j < S) acc = fmaf(wt_s[h * kMergeSplits + s0 + j], v[j], acc);
+        }
+        const float den = den_s[h];
+        out[e] = (E)(den == 0.f ? 0.f : acc / den);
+    }
+}
+
+template <typename E, int D, int KG, int NW, bool SCORES>
+__global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedParams p)
+{
+    constexpr int kSteps = D / 32;                        // matrix instructions per sub-tile of keys
+    constexpr int kVE = D / 16;                           // channels of a value row that a lane loads
+    constexpr int kVW = kVE / 2;                          // .. in 32-bit words
+    typedef typename Vec<E>::v8 vec8;
+    constexpr int kJoin = NW * KG * (D + 2), kMerge = 4 + KG * (kMergeSplits + 1);
+    __shared__ __align__(16) float lds[kJoin > kMerge ? kJoin : kMerge];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int kg = lane >> 4, c = lane & 15, G = p.G;
+    const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+    const size_t bg = (size_t)b * p.Hkv + g, row0 = (size_t)b * p.Hq + (size_t)g * G;
+    arrival_t seen = 0;
+    if (p.S > 1 && t == 0) seen = arrival_peek(p.words + bg);
+
+    const int len = clamped_len(p.seq_lens, b, p.N);
+    int chunk = (int)(((long long)len + p.S - 1) / p.S);
+    chunk = (chunk + kTokens - 1) / kTokens * kTokens;
+    const long long first = (long long)split * chunk;
+    const int n0 = (int)(first < len ? first : len), n1 = (int)(first + chunk < len ? first + chunk : len);
+
+    vec8 qf[kSteps];
+    {
+        const char *const row = p.q + b * p.q_b + (long long)(g * G + (c < G ? c : 0)) * p.q_h;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            const uint4 x = reinterpret_cast<const uint4 *>(row)[4 * j + kg];
+            qf[j] = c < G ? __builtin_bit_cast(vec8, x) : as_vec<E>(0, 0, 0, 0);
+        }
+    }
+
+    const int32_t *const pages = p.block_table + b * p.max_pages;
+    const int shift = p.pages.shift, last_col = (p.N - 1) >> shift;
+    const unsigned slot_mask = (1u << shift) - 1;
+    const char *const k0 = p.pages.k + (size_t)g * p.pages.k_head, *const v0 = p.pages.v + (size_t)g * p.pages.v_head;
+    const int krow = 8 * (c >> 2) + (c & 3);              // this lane's key token of sub-tile 0; of sub-tile 1: + 4
+    auto page_at = [&](int tok) {
+        const int col = tok >> shift;
+        return pages[col < last_col ? col : last_col];
+    };
+
+    float m = -INFINITY, l = 0.f;
+    floatx4 acc[kVE];
+#pragma unroll
+    for (int i = 0; i < kVE; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    int t0 = n0 + wave * kTokens;
+    int next_k = 0, next_v = 0;
+    if (t0 < n1) {
+        next_k = page_at(t0 + krow);
+        next_v = page_at(t0 + 8 * kg);
+    }
+    for (; t0 < n1; t0 += NW * kTokens) {
+        const unsigned page_k = (unsigned)next_k, page_v = (unsigned)next_v;
+        const bool there = page_v < p.pages.num_pages;
+        uint4 kr[2][kSteps];
+        unsigned vr[8][kVW];
+        {
+            const char *row = k0 + (size_t)(page_k < p.pages.num_pages ? page_k : 0u) * p.pages.k_page +
+                              (size_t)((unsigned)(t0 + krow) & slot_mask) * p.pages.k_slot + 16 * kg;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) kr[u][j] = *reinterpret_cast<const uint4 *>(row + 64 * j);
+                row += 4 * (size_t)p.pages.k_slot;
+            }
+        }
+        {
+            const char *row = v0 + (size_t)(there ? page_v : 0u) * p.pages.v_page +
+                              (size_t)((unsigned)(t0 + 8 * kg) & slot_mask) * p.pages.v_slot + 2 * kVE * c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (kVW == 4) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(row);
+                    vr[j][0] = x.x; vr[j][1] = x.y; vr[j][2] = x.z; vr[j][3] = x.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(row);
+                    vr[j][0] = x.x; vr[j][1] = x.y;
+                }
+                row += p.pages.v_slot;
+            }
+        }
+        const int tn = t0 + NW * kTokens;
+        if (tn < n1) {
+            next_k = page_at(tn + krow);
+            next_v = page_at(tn + 8 * kg);
+        }
+
+        // ---- scores, in log2 units: head c, tokens t0 + 8 kg + e
+        float s[8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            floatx4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) d = Vec<E>::mfma(__builtin_bit_cast(vec8, kr[u][j]), qf[j], d);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[4 * u + r] = d[r] * p.scale2;
+        }
+        // A tile with a hole, or the sequence's last: what is not there has no score, and whatever its rows hold (an
+        // infinity times a probability of 0 is NaN) is taken out.
+        if (t0 + kTokens > n1 || !__all(there)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool in = there && t0 + 8 * kg + e < n1;
+                s[e] = in ? s[e] : -INFINITY;
+#pragma unroll
+                for (int w = 0; w < kVW; ++w) vr[e][w] = in ? vr[e][w] : 0u;
+            }
+        }
+        if constexpr (SCORES) {
+            if (c < G) {
+                float *const to = p.scores + (row0 + c) * p.n_pad + t0 + 8 * kg;
+                reinterpret_cast<float4 *>(to)[0] = make_float4(s[0], s[1], s[2], s[3]);
+                reinterpret_cast<float4 *>(to)[1] = make_float4(s[4], s[5], s[6], s[7]);
+            }
+        }
+
+        // ---- softmax: every lane of a head has the same maximum, and a sum of its own tokens
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
+        top = rows_max(top);
+        if (__any(top > m)) {
+            const float to = fmaxf(m, top);
+            const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - to) : 0.f;
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < kVE; ++i) acc[i] *= f;
+        }
+        const float base = (m > -INFINITY ? m : 0.f) - Vec<E>::kLift;
+        vec8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = __builtin_amdgcn_exp2f(s[e] - base);
+            l += x;
+            hi[e] = (E)x;
+            lo[e] = (E)(x - (float)hi[e]);
+        }
+
+        // ---- output
+#pragma unroll
+        for (int i = 0; i < kVE; ++i) {
+            const unsigned pick = i & 1 ? 0x07060302u : 0x05040100u;       // high or low halves of two rows' words
+            vec8 a = as_vec<E>(__builtin_amdgcn_perm(vr[1][i / 2], vr[0][i / 2], pick), __builtin_amdgcn_perm(vr[3][i / 2], vr[2][i / 2], pick),
+                               __builtin_amdgcn_perm(vr[5][i / 2], vr[4][i / 2], pick), __builtin_amdgcn_perm(vr[7][i / 2], vr[6][i / 2], pick));
+            acc[i] = Vec<E>::mfma(a, hi, acc[i]);
+            acc[i] = Vec<E>::mfma(a, lo, acc[i]);
+        }
+    }
+
+    // ---- the wavefronts join
+    l = rows_sum(l);
+    float *const o_s = lds, *const m_s = lds + NW * KG * D, *const l_s = m_s + NW * KG;
+    if (c < G) {
+        float *const to = o_s + (wave * KG + c) * D;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < kVE; i += 4)
+                *reinterpret_cast<float4 *>(to + (4 * kg + r) * kVE + i) = make_float4(acc[i][r], acc[i + 1][r], acc[i + 2][r], acc[i + 3][r]);
+        if (kg == 0) {
+            m_s[wave * KG + c] = m;
+            l_s[wave * KG + c] = l;
+        }
+    }
+    __syncthreads();
+    for (int e = t; e < G * D; e += NW * 64) {
+        const int h = e / D, ch = e - h * D;
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, m_s[w * KG + h]);
+        const float at = M > -INFINITY ? M : 0.f;
+        float den = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(m_s[w * KG + h] - at);
+            den = fmaf(f, l_s[w * KG + h], den);
+            o = fmaf(f, o_s[(w * KG + h) * D + ch], o);
+        }
+        if (p.S == 1) {
+            static_cast<E *>(p.out)[(row0 + h) * D + ch] = (E)(den == 0.f ? 0.f : o / den);
+            if (ch == 0) {
+                const float total = den == 0.f ? -INFINITY : M - Vec<E>::kLift + log2f(den);
+                if (p.lse) p.lse[row0 + h] = natural(total);
+                if (p.lse2) p.lse2[row0 + h] = total;
+            }
+        } else {
+            const size_t at_s = (bg * p.S + split) * G + h;
+            shared_store(p.part_o + at_s * D + ch, o);
+            if (ch == 0) {
+                shared_store(p.part_m + at_s, M - Vec<E>::kLift);
+                shared_store(p.part_l + at_s, den);
+            }
+        }
+    }
+    if (p.S == 1) return;
+    if (t == 0) arrival_open(p.words + bg, seen, p.nonce);
+    merge_last<E, D, KG, NW>(p, lds, bg, row0);
+}
+
+// The step's attention weights, summed over the heads of a KV head, onto the sums of its tokens.
+__global__ __launch_bounds__(256) void paged_weights_kernel(const PagedParams p)
+{
+    const int g = blockIdx.y, b = blockIdx.z;
+    const int len = clamped_len(p.seq_lens, b, p.N);
+    const size_t row0 = (size_t)b * p.Hq + (size_t)g * p.G;
+    const long long t = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (t >= len) return;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int h = 0; h < p.G; ++h) {
+        const float4 s = *reinterpret_cast<const float4 *>(p.scores + (row0 + h) * p.n_pad + t);
+        const float total = p.lse2[row0 + h];
+        const float at = total > -INFINITY || total != total ? total : 0.f;       // nothing attended to: weights 0
+        sum.x += __builtin_amdgcn_exp2f(s.x - at);
+        sum.y += __builtin_amdgcn_exp2f(s.y - at);
+        sum.z += __builtin_amdgcn_exp2f(s.z - at);
+        sum.w += __builtin_amdgcn_exp2f(s.w - at);
+    }
+    const float *const in = p.w_in ? p.w_in + ((size_t)b * p.Hkv + g) * p.w_cap + t : nullptr;
+    float *const out = p.w_out + ((size_t)b * p.Hkv + g) * p.w_cap + t;
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (t + i < len) out[i] = (in ? in[i] : 0.f) + v[i];
+}
+
+template <typename E, int D>
+void start(const PagedParams &p, hipStream_t stream)
+{
+    constexpr int NW = 8;
+    const dim3 grid((unsigned)p.S, (unsigned)p.Hkv, (unsigned)p.B), block(NW * 64);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p); };
+    if (p.scores)
+        p.G <= 4 ? go(paged_attention_kernel<E, D, 4, NW, true>) : go(paged_attention_kernel<E, D, 16, NW, true>);
+    else
+        p.G <= 4 ? go(paged_attention_kernel<E, D, 4, NW, false>) : go(paged_attention_kernel<E, D, 16, NW, false>);
+}
+
+} // namespace
+
+int launch_paged_attention(const PagedParams &p, int is_bf16, int D, hipStream_t stream)
+{
+    if (is_bf16)
+        D == 128 ? start<bf16, 128>(p, stream) : start<bf16, 64>(p, stream);
+    else
+        D == 128 ? start<f16, 128>(p, stream) : start<f16, 64>(p, stream);
+    return hipGetLastError() == hipSuccess ? 0 : -4;
+}
+
+int launch_paged_weights(const PagedParams &p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((p.N + 1023) / 1024), (unsigned)p.Hkv, (unsigned)p.B);
+    hipLaunchKernelGGL(paged_weights_kernel, grid, dim3(256), 0, stream, p);
+    return hipGetLastError() == hipSuccess ? 0 : -4;
+}
+
+} // namespace vecinfer
