@@ -155,6 +155,10 @@ class Rotary:
         return _RotaryCfg(self.head_dim, self.rot_dim, self.interleaved, self.scaling, self.base, self.factor, self.low_turns,
                           self.high_turns, self.orig_len, self.magnitude)
 
+    @_once
+    def _p(self) -> int:
+        return C.addressof(self._c)
+
     def __getstate__(self):
         return {f: self.__dict__[f] for f in self.__dataclass_fields__}
 
@@ -172,6 +176,7 @@ class Pages:
         self.num_pages, self.num_kv_heads, self.page_size, self.head_dim = k.shape
         self._c = _Pages(k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], self.head_dim, self.num_kv_heads, self.page_size,
                          self.num_pages, _steps(k, "k", True), _steps(v, "v", True))
+        self._p, self._dev = C.addressof(self._c), k.device.index
 
 
 def _steps(t: torch.Tensor, name: str, written: bool):
@@ -282,6 +287,8 @@ def _bind_fast(L: C.CDLL) -> None:
     if m.torch_version == torch.__version__.split("+")[0]:
         m.bind(*(C.cast(getattr(L, "vecinfer_" + n), C.c_void_p).value for n in (
             "encode_keys", "encode_values", "append_kv", "decode_attention", "decode_attention_residual", "decode_step")), _stream)
+        m.bind_paged(*(C.cast(getattr(L, "vecinfer_" + n), C.c_void_p).value for n in (
+            "rotary", "paged_append", "paged_attention", "paged_evict")), _stream_on)
         _fast = m
 
 
@@ -314,6 +321,13 @@ def _stream(stream) -> int:
     if stream is None:
         return _raw_stream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _stream_on(stream, device: int) -> int:
+    """_stream for work on tensors of that device, which has to be the current one."""
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return _raw_stream(device) if stream is None else _stream(stream)
 
 
 def vecinfer_encode_keys(cfg: Config, k_f16, lam, cb_k, k_idx, pos0: int = 0, stream=None) -> None:
@@ -628,6 +642,10 @@ def new_rotary_table(rot: Rotary, freqs=None, device="cuda") -> torch.Tensor:
 def vecinfer_rotary(rot: Rotary, table, x, out, positions=None, pos0: int = 0, inverse: int = 0, stream=None) -> None:
     """Turn x [B, H, T, D] (fp16 or bf16, any strides) into out by its positions: int32 [B, T], or pos0 + t.  out may be
     x.  inverse: turn back, which takes the gradient of out to that of x."""
+    if _fast is not None and type(rot) is Rotary:
+        rc = _fast.rotary(rot._p, table, x, out, positions, pos0, inverse, stream)
+        if rc is not None:
+            return _check(rc)
     if not isinstance(x, torch.Tensor) or x.dim() != 4 or x.dtype not in _TYPES:
         raise ValueError("x: expected fp16 or bf16 [B, H, T, D]")
     B, H, T, D = x.shape
@@ -643,6 +661,11 @@ def vecinfer_paged_append(pages: Pages, k_new, v_new, block_table, seq_lens, new
     """Write T new tokens per sequence, k_new and v_new [B, Hkv, T, D], to their pages (block_table int32 [B, max_pages]),
     keys turned by `rot`; turn the queries q [B, Hq, T, D] into q_out.  seq_lens [B] count the new tokens, of which
     sequence b has new_lens[b] (or T)."""
+    if _fast is not None and type(pages) is Pages and (rot is None or type(rot) is Rotary):
+        rc = _fast.paged_append(pages._p, pages._dev, None if rot is None else rot._p, table, k_new, v_new, q, q_out, block_table,
+                                seq_lens, new_lens, positions, weights, stream)
+        if rc is not None:
+            return _check(rc)
     pool, dtype = _pool(pages, "pages"), pages.k.dtype
     B, Hkv, T, D = k_new.shape
     shape = (B, pages.num_kv_heads, T, pages.head_dim)
@@ -683,6 +706,11 @@ def vecinfer_paged_attention(pages: Pages, q, block_table, workspace, out, lse=N
     """Attention of one new token per sequence, q [B, Hq, D] (any strides), over its pages; writes out [B, Hq, D] (and lse
     [B, Hq]).  scale: 1 / sqrt(D) unless given.  weights_out [B, Hkv, w_cap] = weights_in (or 0) + the attention weights
     of the step, summed over the heads of a KV head; weights_in may be weights_out."""
+    if _fast is not None and type(pages) is Pages:
+        rc = _fast.paged_attention(pages._p, pages._dev, q, block_table, workspace, out, lse, seq_lens, N, scale, num_splits,
+                                   weights_in, weights_out, stream)
+        if rc is not None:
+            return _check(rc)
     pool = _pool(pages, "pages")
     B, Hq, D = q.shape
     dtype = pages.k.dtype
@@ -720,6 +748,11 @@ def vecinfer_paged_evict(pages: Pages, weights, block_table, dst_pages: Pages, d
     [B, Hkv, w_cap], `keep` in all, in order, in the pages of dst_table [B, dst_max_pages] (of `dst_pages`, which may be
     `pages`; not pages that are read).  Writes dst_lens [B] and, if given, dst_weights [B, Hkv, dst_w_cap] and the kept
     tokens' old indices, kept [B, Hkv, keep].  N: as many tokens as weights has, at most, unless given."""
+    if _fast is not None and type(pages) is Pages and type(dst_pages) is Pages:
+        rc = _fast.paged_evict(pages._p, pages._dev, weights, block_table, dst_pages._p, dst_pages._dev, dst_table, dst_lens, workspace,
+                               keep, first, recent, seq_lens, N, dst_weights, kept, stream)
+        if rc is not None:
+            return _check(rc)
     src, dst = _pool(pages, "pages"), _pool(dst_pages, "dst_pages")
     B, max_pages = block_table.shape
     Hkv, w_cap = pages.num_kv_heads, weights.shape[-1]

@@ -27,7 +27,12 @@ decltype(&vecinfer_append_kv) append_kv;
 decltype(&vecinfer_decode_attention) decode_attention;
 decltype(&vecinfer_decode_attention_residual) decode_residual;
 decltype(&vecinfer_decode_step) decode_step;
+decltype(&vecinfer_rotary) rotary_call;
+decltype(&vecinfer_paged_append) paged_append_call;
+decltype(&vecinfer_paged_attention) paged_attention_call;
+decltype(&vecinfer_paged_evict) paged_evict_call;
 PyObject *find_stream;                   // binding._stream
+PyObject *find_stream_on;                // binding._stream_on
 
 struct Refused {};                       // an argument that the interpreter's checks have to look at
 struct Raised {};                        // Python's error is set
@@ -254,8 +259,235 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// ---- the paged cache and rotary positions
+
+// What a call needs of its pages, and of the device that they are on.
+struct Pool {
+    const vecinfer_pages *p;
+    at::ScalarType type;
+    int64_t D, Hkv, device;
+    Pool(PyObject *o, PyObject *dev) : p(static_cast<const vecinfer_pages *>(address(o))), device(integer(dev))
+    {
+        if (!p) throw Refused();
+        type = p->dtype == VECINFER_BF16 ? at::kBFloat16 : at::kHalf;
+        D = p->head_dim;
+        Hkv = p->num_kv_heads;
+    }
+};
+
+void on(const at::Tensor &t, int64_t device)
+{
+    if (!t.is_cuda() || t.get_device() != device) throw Refused();
+}
+
+// A contiguous tensor on that device, or None.
+template <typename T>
+T *flat(PyObject *o, int64_t device, at::ScalarType type, std::initializer_list<int64_t> shape)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    on(t, device);
+    return static_cast<T *>(pointer(t, type, shape));
+}
+
+// A tensor of any strides with adjacent channels, and the strides of its other axes (an axis of one index has none).
+template <int N>
+void *rows(const at::Tensor &t, int64_t device, at::ScalarType type, std::initializer_list<int64_t> shape, int64_t (&steps)[N], bool written = false)
+{
+    on(t, device);
+    if (t.scalar_type() != type || !t.sizes().equals(c10::IntArrayRef(shape)) || t.dim() != N + 1) throw Refused();
+    if (t.size(N) > 1 && t.stride(N) != 1) throw Refused();
+    for (int i = 0; i < N; ++i) {
+        steps[i] = t.size(i) > 1 ? t.stride(i) : 0;
+        if (written && t.size(i) > 1 && steps[i] == 0) throw Refused();
+    }
+    return t.data_ptr();
+}
+
+// The stream for work on that device; raises where it is not the current one.
+void *stream_on(PyObject *o, int64_t device)
+{
+    PyObject *const dev = PyLong_FromLongLong(device);
+    if (!dev) throw Raised();
+    PyObject *const r = PyObject_CallFunctionObjArgs(find_stream_on, o, dev, nullptr);
+    Py_DECREF(dev);
+    if (!r) throw Raised();
+    struct Release {
+        PyObject *r;
+        ~Release() { Py_DECREF(r); }
+    } release{r};
+    return address(r);
+}
+
+int32_t narrow(int64_t v)
+{
+    if (v != (int32_t)v) throw Refused();
+    return (int32_t)v;
+}
+
+// rotary(cfg, table, x, out, positions or None, pos0, inverse, stream)
+PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        if (n != 8) throw Refused();
+        const vecinfer_rotary_cfg *const cfg = static_cast<const vecinfer_rotary_cfg *>(address(a[0]));
+        const at::Tensor &x = tensor(a[2]), &out = tensor(a[3]);
+        const int64_t B = extent(x, 4, 0), H = x.size(1), T = x.size(2), D = cfg->head_dim, dev = x.is_cuda() ? x.get_device() : -1;
+        const at::ScalarType type = x.scalar_type();
+        if (type != at::kHalf && type != at::kBFloat16) throw Refused();
+        int64_t xs[3], os[3];
+        const void *const px = rows(x, dev, type, {B, H, T, D}, xs);
+        void *const po = rows(out, dev, type, {B, H, T, D}, os, true);
+        const uint64_t *const table = reinterpret_cast<const uint64_t *>(flat<int64_t>(a[1], dev, at::kLong, {(int64_t)(cfg->rot_dim / 2)}));
+        const int32_t *const pos = flat<int32_t>(a[4], dev, at::kInt, {B, T});
+        const int64_t pos0 = integer(a[5]);
+        const int32_t b = narrow(B), h = narrow(H), inverse = PyObject_IsTrue(a[6]);
+        if (inverse < 0) throw Raised();
+        void *const stream = stream_on(a[7], dev);
+        return without_gil([&] {
+            return rotary_call(cfg, table, type == at::kBFloat16 ? VECINFER_BF16 : VECINFER_F16, px, xs, po, os, b, h, T, pos, pos0, inverse, stream);
+        });
+    });
+}
+
+// paged_append(pages, device, rot or None, table or None, k_new, v_new, q or None, q_out or None, block_table, seq_lens,
+//              new_lens or None, positions or None, weights or None, stream)
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        if (n != 14) throw Refused();
+        const Pool pool(a[0], a[1]);
+        const int64_t dev = pool.device;
+        const vecinfer_rotary_cfg *const rot = a[2] == Py_None ? nullptr : static_cast<const vecinfer_rotary_cfg *>(address(a[2]));
+        const uint64_t *const table =
+            rot ? reinterpret_cast<const uint64_t *>(flat<int64_t>(a[3], dev, at::kLong, {(int64_t)(rot->rot_dim / 2)})) : nullptr;
+        const at::Tensor &k = tensor(a[4]), &v = tensor(a[5]), &bt = tensor(a[8]);
+        const int64_t B = extent(k, 4, 0), T = k.size(2), cols = extent(bt, 2, 1);
+        int64_t ks[3], vs[3], qs[3], os[3], Hq = 0, w_cap = 0;
+        const void *const pk = rows(k, dev, pool.type, {B, pool.Hkv, T, pool.D}, ks), *const pv = rows(v, dev, pool.type, {B, pool.Hkv, T, pool.D}, vs);
+        if ((a[6] == Py_None) != (a[7] == Py_None)) throw Refused();
+        const void *pq = nullptr;
+        void *po = nullptr;
+        if (a[6] != Py_None) {
+            const at::Tensor &q = tensor(a[6]);
+            Hq = extent(q, 4, 1);
+            pq = rows(q, dev, pool.type, {B, Hq, T, pool.D}, qs);
+            po = rows(tensor(a[7]), dev, pool.type, {B, Hq, T, pool.D}, os, true);
+        }
+        const int32_t *const pages = flat<int32_t>(a[8], dev, at::kInt, {B, cols}), *const lens = flat<int32_t>(a[9], dev, at::kInt, {B});
+        const int32_t *const fresh = flat<int32_t>(a[10], dev, at::kInt, {B}), *const pos = flat<int32_t>(a[11], dev, at::kInt, {B, T});
+        if (a[12] != Py_None) w_cap = extent(tensor(a[12]), 3, 2);
+        float *const w = flat<float>(a[12], dev, at::kFloat, {B, pool.Hkv, w_cap});
+        const int32_t b = narrow(B), hq = narrow(Hq);
+        void *const stream = stream_on(a[13], dev);
+        return without_gil([&] {
+            return paged_append_call(pool.p, rot, table, pk, ks, pv, vs, pq, qs, po, os, hq, pages, cols, lens, fresh, pos, b, T, w, w_cap, stream);
+        });
+    });
+}
+
+// paged_attention(pages, device, q, block_table, workspace, out, lse or None, seq_lens or None, N or None, scale or None,
+//                 num_splits, weights_in or None, weights_out or None, stream)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        if (n != 14) throw Refused();
+        const Pool pool(a[0], a[1]);
+        const int64_t dev = pool.device;
+        const at::Tensor &q = tensor(a[2]), &bt = tensor(a[3]), &ws = tensor(a[4]);
+        const int64_t B = extent(q, 3, 0), Hq = q.size(1), cols = extent(bt, 2, 1);
+        int64_t qs[2], w_cap = 0;
+        const void *const pq = rows(q, dev, pool.type, {B, Hq, pool.D}, qs);
+        const int32_t *const pages = flat<int32_t>(a[3], dev, at::kInt, {B, cols});
+        on(ws, dev);
+        if (!ws.is_contiguous()) throw Refused();
+        void *const wp = ws.data_ptr();
+        const size_t wb = (size_t)ws.numel() * ws.element_size();
+        if (a[5] == Py_None) throw Refused();
+        void *const out = flat<void>(a[5], dev, pool.type, {B, Hq, pool.D});
+        float *const lse = flat<float>(a[6], dev, at::kFloat, {B, Hq});
+        const int32_t *const lens = flat<int32_t>(a[7], dev, at::kInt, {B});
+        const int64_t N = a[8] == Py_None ? cols * pool.p->page_size : integer(a[8]);
+        double scale = 0;
+        if (a[9] == Py_None)
+            scale = pool.D == 64 ? 0.125 : 0.08838834764831845;            // 1 / sqrt(D)
+        else if (PyFloat_CheckExact(a[9]))
+            scale = PyFloat_AS_DOUBLE(a[9]);
+        else
+            throw Refused();
+        const int32_t splits = integer32(a[10]);
+        if (a[12] == Py_None && a[11] != Py_None) throw Refused();
+        if (a[12] != Py_None) w_cap = extent(tensor(a[12]), 3, 2);
+        const float *const w_in = flat<float>(a[11], dev, at::kFloat, {B, pool.Hkv, w_cap});
+        float *const w_out = flat<float>(a[12], dev, at::kFloat, {B, pool.Hkv, w_cap});
+        const int32_t b = narrow(B), hq = narrow(Hq);
+        void *const stream = stream_on(a[13], dev);
+        return without_gil([&] {
+            return paged_attention_call(pool.p, pq, qs, hq, pages, cols, lens, b, N, (float)scale, splits, wp, wb, out, lse, w_in, w_out, w_cap, stream);
+        });
+    });
+}
+
+// paged_evict(pages, device, weights, block_table, dst_pages, dst_device, dst_table, dst_lens, workspace, keep, first, recent,
+//             seq_lens or None, N or None, dst_weights or None, kept or None, stream)
+PyObject *paged_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        if (n != 17) throw Refused();
+        const Pool src(a[0], a[1]), dst(a[4], a[5]);
+        const int64_t dev = src.device;
+        if (dst.device != dev) throw Refused();
+        const at::Tensor &w = tensor(a[2]), &bt = tensor(a[3]), &dt = tensor(a[6]), &ws = tensor(a[8]);
+        const int64_t B = extent(bt, 2, 0), cols = bt.size(1), dcols = extent(dt, 2, 1), w_cap = extent(w, 3, 2);
+        const float *const pw = flat<float>(a[2], dev, at::kFloat, {B, src.Hkv, w_cap});
+        const int32_t *const pages = flat<int32_t>(a[3], dev, at::kInt, {B, cols}), *const dpages = flat<int32_t>(a[6], dev, at::kInt, {B, dcols});
+        if (a[7] == Py_None) throw Refused();
+        int32_t *const dlens = flat<int32_t>(a[7], dev, at::kInt, {B});
+        on(ws, dev);
+        if (!ws.is_contiguous()) throw Refused();
+        void *const wp = ws.data_ptr();
+        const size_t wb = (size_t)ws.numel() * ws.element_size();
+        const int64_t keep = integer(a[9]), first = integer(a[10]), recent = integer(a[11]), all = cols * src.p->page_size;
+        const int32_t *const lens = flat<int32_t>(a[12], dev, at::kInt, {B});
+        const int64_t N = a[13] == Py_None ? (w_cap < all ? w_cap : all) : integer(a[13]);
+        const int64_t dw_cap = a[14] == Py_None ? 0 : extent(tensor(a[14]), 3, 2);
+        float *const dw = flat<float>(a[14], dev, at::kFloat, {B, src.Hkv, dw_cap});
+        int32_t *const kept = flat<int32_t>(a[15], dev, at::kInt, {B, src.Hkv, keep});
+        const int32_t b = narrow(B);
+        void *const stream = stream_on(a[16], dev);
+        return without_gil([&] {
+            return paged_evict_call(src.p, pw, w_cap, pages, cols, lens, b, N, keep, first, recent, dst.p, dpages, dcols, dlens, dw, dw_cap, kept, wp, wb,
+                                    stream);
+        });
+    });
+}
+
+// bind_paged(addresses of the library's functions, in the order of the variables above, then the function for streams)
+PyObject *bind_paged(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "bind_paged: four addresses and a function");
+        return nullptr;
+    }
+    void *p[4];
+    for (int i = 0; i < 4; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    Py_INCREF(a[4]);
+    Py_XDECREF(find_stream_on);
+    find_stream_on = a[4];
+    rotary_call = reinterpret_cast<decltype(rotary_call)>(p[0]);
+    paged_append_call = reinterpret_cast<decltype(paged_append_call)>(p[1]);
+    paged_attention_call = reinterpret_cast<decltype(paged_attention_call)>(p[2]);
+    paged_evict_call = reinterpret_cast<decltype(paged_evict_call)>(p[3]);
+    Py_RETURN_NONE;
+}
+
 #define VECINFER_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {VECINFER_METHOD(bind), VECINFER_METHOD(encode), VECINFER_METHOD(append), VECINFER_METHOD(decode),
+                         VECINFER_METHOD(bind_paged), VECINFER_METHOD(rotary), VECINFER_METHOD(paged_append), VECINFER_METHOD(paged_attention),
+                         VECINFER_METHOD(paged_evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
