@@ -2,14 +2,14 @@
 // move to pages of their own, in order.
 //
 // The choice: every token has a 32-bit key in the order of its weight; the first and the most recent ones have the
-// largest key of all, tokens of a hole have key 0 and never stay.  One workgroup per (sequence, KV head) looks for the
-// key T of the last one that stays, by digits of 11, 11 and 10 bits, and reads the row three times: a histogram of the
-// first digit; then, of the tokens that have T's first digit, the other bits into a list in LDS, from which the other two
-// digits are found; then the tokens above T, and as many of those equal to it, lowest index first, as there is room for,
-// are listed in order.  Each of the 16 wavefronts takes a stretch of the row in the second and third reading, so that
-// the third knows where each has to start.  (A list that does not fit, thousands of equal weights say, stays where it is:
-// the row is read again for each digit.)
-// What bounds it is one compute unit's reading and counting: PLACEHOLDER_FIGURES
+// largest key of all, tokens of a hole have key 0 and never stay.  The key T of the last one that stays is found by
+// digits of 11, 11 and 10 bits: a histogram of the tokens that agree with T so far, and the bin at which, counted from the
+// top, the room ends.  Then the tokens above T, and as many of those equal to it, lowest index first, as there is room for,
+// are listed in order.
+// What bounds it is issue: some 70 vector instructions per token, of which one compute unit does 64 lanes per cycle.  So a
+// row of up to kHeld tokens, whose keys fit a workgroup's registers, is one workgroup's in one launch, and a longer one is
+// cut into up to kMaxParts stretches, a launch per digit and one for the list, through a histogram per stretch: each
+// workgroup of the next launch adds them up for itself, which needs no atomics, no clearing and no order of workgroups.
 // The move: 16 lanes per row of a kept token, keys and values.
 #include "paged.h"
 
@@ -19,8 +19,12 @@ namespace {
 
 constexpr int kSelect = 1024, kWaves = kSelect / 64;
 constexpr int kBins = 2048;
-constexpr int kCopies = 4;                                // of a histogram: lanes of neighbouring tokens count apart
-constexpr int kList = 24576;                              // tokens of T's first digit that LDS has room for
+constexpr int kCopies = 4;                                // of a histogram in LDS: neighbouring lanes count apart
+constexpr int kTurns = 4;                                 // of 256 tokens per wavefront whose keys are held in registers
+constexpr int kHeld = kSelect * 4 * kTurns;               // tokens of a workgroup that are read once
+constexpr int kPart = kHeld / 2;                          // tokens of a stretch, unless that makes too many
+constexpr int kMaxParts = 64;
+constexpr int kGroup = 32, kGroups = kBins / kGroup, kHist = kBins + kGroups;    // a stretch's histogram in memory
 
 // Order of weights as unsigned numbers: -inf < .. < -0 = 0 < .. < inf; what is no number comes below all.
 __device__ __forceinline__ unsigned weight_key(float w)
@@ -34,45 +38,119 @@ struct __attribute__((packed, aligned(4))) Four {
     float v[4];
 };
 
-struct Row {
+struct Shared {
+    unsigned hist[kBins * kCopies];
+    unsigned above[kWaves], equal[kWaves], sums[kWaves];
+    unsigned pick[2];
+    unsigned all[kWaves][kGroups], mine[kWaves][kGroups];
+};
+
+// What a workgroup knows of its tokens [from, to) of a row, of which this wavefront has [mine, mine_to).
+struct Stretch {
     const float *w;
     const int32_t *pages;
     unsigned num_pages;
     int shift, len, first, recent_from;
+    int mine, mine_to;
+    bool held;                                            // k has all the keys
+    unsigned k[kTurns][4];
+
+    // The keys of tokens i .. i + 3 (i a multiple of 4: they share a page); behind the end: 0.
+    __device__ __forceinline__ void keys4(int i, unsigned (&key)[4]) const
+    {
+        key[0] = key[1] = key[2] = key[3] = 0u;
+        if (i >= mine_to) return;
+        const unsigned page = (unsigned)pages[i >> shift];
+        Four f;
+        if (i + 3 < mine_to) {
+            f = *reinterpret_cast<const Four *>(w + i);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f.v[e] = i + e < mine_to ? w[i + e] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            key[e] = i + e < first || i + e >= recent_from ? 0xffffffffu : weight_key(f.v[e]);
+            if (page >= num_pages || i + e >= mine_to) key[e] = 0u;
+        }
+    }
+    __device__ __forceinline__ void read(int from)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int a = 0; a < kTurns; ++a) keys4(from + 256 * a + 4 * lane, k[a]);
+    }
+    __device__ __forceinline__ void open(const EvictParams &p, int g, int b, int part, int parts)
+    {
+        const size_t bg = (size_t)b * p.Hkv + g;
+        w = p.w + bg * p.w_cap;
+        pages = p.block_table + b * p.max_pages;
+        num_pages = p.src.num_pages;
+        shift = p.src.shift;
+        len = clamped_len(p.seq_lens, b, p.N);
+        first = p.first;
+        recent_from = len - p.recent;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        const long long stretch = parts * kWaves, step = ((long long)len + 256 * stretch - 1) / (256 * stretch) * 256;
+        const long long at = (part * kWaves + wave) * step;
+        mine = (int)(at < len ? at : len);
+        mine_to = (int)(at + step < len ? at + step : len);
+        held = step <= 256 * kTurns;
+        if (held) read(mine);
+    }
+    // f(first token, keys) for the lane's fours of this wavefront's tokens, in order
+    template <typename F>
+    __device__ __forceinline__ void each(F &&f)
+    {
+        const int lane = threadIdx.x & 63;
+        for (int i = mine; i < mine_to; i += 256 * kTurns) {
+            if (!held) read(i);
+#pragma unroll
+            for (int a = 0; a < kTurns; ++a)
+                if (i + 256 * a < mine_to) f(i + 256 * a + 4 * lane, k[a]);
+        }
+    }
 };
 
-// The keys of tokens i .. i + 3 (i a multiple of 4: they share a page); behind the end: 0.
-__device__ __forceinline__ void keys4(const Row &r, int i, unsigned (&k)[4])
+__device__ __forceinline__ void clear_hist(Shared &s)
 {
-    k[0] = k[1] = k[2] = k[3] = 0u;
-    if (i >= r.len) return;
-    const unsigned page = (unsigned)r.pages[i >> r.shift];
-    Four f;
-    if (i + 3 < r.len) {
-        f = *reinterpret_cast<const Four *>(r.w + i);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f.v[e] = i + e < r.len ? r.w[i + e] : 0.f;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        k[e] = i + e < r.first || i + e >= r.recent_from ? 0xffffffffu : weight_key(f.v[e]);
-        if (page >= r.num_pages || i + e >= r.len) k[e] = 0u;
-    }
+    static_assert(kCopies == 4, "16 bytes per bin");
+    for (int i = threadIdx.x; i < kBins; i += kSelect) reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
 }
 
-// f(keys) for the tokens [from, to), 256 per wavefront and turn, `step` tokens apart; four turns are requested together.
-template <typename F>
-__device__ __forceinline__ void each(const Row &r, int from, int to, int step, F &&f)
+// Histogram of the next digit over the tokens whose digits so far are `prefix`.  Ends behind a barrier.
+template <int DIGIT>
+__device__ __forceinline__ void count_digit(Shared &s, Stretch &x, unsigned prefix)
 {
-    constexpr int kAhead = 4;
-    for (int i = from; i < to; i += kAhead * step) {
-        unsigned k[kAhead][4];
+    constexpr int kAt = DIGIT == 1 ? 21 : (DIGIT == 2 ? 10 : 0);
+    constexpr unsigned kMask = DIGIT == 3 ? 1023u : 2047u;
+    const int copy = threadIdx.x & (kCopies - 1);
+    clear_hist(s);
+    __syncthreads();
+    x.each([&](int, const unsigned(&k)[4]) {
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) keys4(r, i + a * step < to ? i + a * step + 4 * (int)(threadIdx.x & 63) : r.len, k[a]);
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (DIGIT == 1) {
+                // (what is always kept comes by the wavefront, and would queue for one place)
+                const unsigned long long always = __ballot(k[e] == 0xffffffffu);
+                if (always && (threadIdx.x & 63) == 0) atomicAdd(&s.hist[(kBins - 1) * kCopies], (unsigned)__popcll(always));
+                if (k[e] && k[e] != 0xffffffffu) atomicAdd(&s.hist[(k[e] >> kAt) * kCopies + copy], 1u);
+            } else {
+                if (k[e] && k[e] >> (DIGIT == 2 ? 21 : 10) == prefix) atomicAdd(&s.hist[(k[e] >> kAt & kMask) * kCopies + copy], 1u);
+            }
+        }
+    });
+    __syncthreads();
+}
+
+// This thread's two bins, the upper one first.
+__device__ __forceinline__ void own_bins(const Shared &s, unsigned (&h)[2])
+{
+    static_assert(kBins == 2 * kSelect, "two bins per thread");
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (i + a * step < to) f(i + a * step + 4 * (int)(threadIdx.x & 63), k[a]);
+    for (int i = 0; i < 2; ++i) {
+        const uint4 c = reinterpret_cast<const uint4 *>(s.hist)[kBins - 1 - (2 * (int)threadIdx.x + i)];
+        h[i] = c.x + c.y + c.z + c.w;
     }
 }
 
@@ -86,28 +164,17 @@ __device__ __forceinline__ unsigned wave_prefix(unsigned v, int lane)       // i
     return v;
 }
 
-struct Shared {
-    unsigned hist[kBins * kCopies];
-    unsigned list[kList];
-    unsigned above[kWaves], equal[kWaves], sums[kWaves];
-    unsigned listed, pick[3];
-};
-
-// The bin at which, counted from the top, the room ends: in pick[0]; the tokens above it in pick[1], in it in pick[2].
-// pick[0] = kBins: there is room for all.  Called by all threads, histogram complete; ends behind a barrier.
-__device__ __forceinline__ void find_bin(Shared &s, unsigned room)
+// The bin (h: this thread's two) at which, counted from the top, the room ends: returned, and the tokens above it taken
+// off the room; kBins: there is room for all.  Called by all threads, ends behind a barrier.
+__device__ __forceinline__ unsigned find_bin(Shared &s, const unsigned (&h)[2], unsigned &room)
 {
-    static_assert(kBins == 2 * kSelect, "two bins per thread");
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    unsigned h[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint4 c = reinterpret_cast<const uint4 *>(s.hist)[kBins - 1 - (2 * t + i)];
-        h[i] = c.x + c.y + c.z + c.w;
-    }
     const unsigned upto = wave_prefix(h[0] + h[1], lane);
     if (lane == 63) s.sums[wave] = upto;
-    if (t == 0) s.pick[0] = kBins;
+    if (t == 0) {
+        s.pick[0] = kBins;
+        s.pick[1] = 0;
+    }
     __syncthreads();
     unsigned before = upto - h[0] - h[1];
     for (int w = 0; w < wave; ++w) before += s.sums[w];
@@ -116,148 +183,116 @@ __device__ __forceinline__ void find_bin(Shared &s, unsigned room)
         if (before <= room && room < before + h[i]) {     // (one bin of all)
             s.pick[0] = kBins - 1 - (2 * t + i);
             s.pick[1] = before;
-            s.pick[2] = h[i];
         }
         before += h[i];
     }
     __syncthreads();
+    const unsigned bin = s.pick[0];
+    room -= s.pick[1];
+    return bin;
 }
 
-__device__ __forceinline__ void clear_hist(Shared &s)
+// find_bin over the sum of the stretches' histograms in memory; and of the stretches before `part`, how many tokens lie
+// above the bin and in it.  First the group of bins in which the room ends, by the sums, then the bin in it, so that a
+// workgroup reads 384 bytes of each stretch and not 8 KB (all bins of 13 stretches took 5 us more per launch).
+__device__ __forceinline__ unsigned find_bin_of_parts(Shared &s, const unsigned *hists, int part, int parts, unsigned &room, unsigned &more,
+                                                      unsigned &same)
 {
-    static_assert(kCopies == 4, "16 bytes per bin");
-    for (int i = threadIdx.x; i < kBins; i += kSelect) reinterpret_cast<uint4 *>(s.hist)[i] = make_uint4(0, 0, 0, 0);
-}
-
-__global__ __launch_bounds__(kSelect) void evict_select_kernel(const EvictParams p)
-{
-    __shared__ __align__(16) Shared s;
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int g = blockIdx.x, b = blockIdx.y;
-    const size_t bg = (size_t)b * p.Hkv + g;
-    Row row;
-    row.w = p.w + bg * p.w_cap;
-    row.pages = p.block_table + b * p.max_pages;
-    row.num_pages = p.src.num_pages;
-    row.shift = p.src.shift;
-    row.len = clamped_len(p.seq_lens, b, p.N);
-    row.first = p.first;
-    row.recent_from = row.len - p.recent;
-    int32_t *const ids = p.ids + bg * (p.keep < p.N ? p.keep : p.N);
-    const int copy = lane & (kCopies - 1);
-    // a wavefront's stretch of the row
-    const int seg = (row.len + 256 * kWaves - 1) / (256 * kWaves) * 256;
-    const int from = wave * seg < row.len ? wave * seg : row.len, to = from + seg < row.len ? from + seg : row.len;
-
-    // ---- T's first digit
-    clear_hist(s);
-    if (t < kWaves) s.above[t] = s.equal[t] = 0;
-    if (t == 0) s.listed = 0;
+    static_assert(kGroups == 64 && kGroup == 32 && kMaxParts * kGroup <= 2 * kSelect, "a lane per group; two rounds of bins");
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    // from the top: lane 0 has the highest group
+    unsigned total = 0, before = 0;
+    for (int q = wave; q < parts; q += kWaves) {
+        const unsigned v = hists[(size_t)q * kHist + kBins + kGroups - 1 - lane];
+        total += v;
+        before += q < part ? v : 0u;
+    }
+    s.all[wave][lane] = total;
+    s.mine[wave][lane] = before;
     __syncthreads();
-    each(row, from, to, 256, [&](int, const unsigned(&k)[4]) {
+    // (every wavefront the same, so that nobody waits for one)
+    total = before = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (k[e]) atomicAdd(&s.hist[(k[e] >> 21) * kCopies + copy], 1u);
-    });
+    for (int w = 0; w < kWaves; ++w) {
+        total += s.all[w][lane];
+        before += s.mine[w][lane];
+    }
+    const unsigned upto = wave_prefix(total, lane), from_top = upto - total, mine_upto = wave_prefix(before, lane);
+    const unsigned long long here = __ballot(from_top <= room && room < upto);
+    if (here == 0) {                                      // there is room for all
+        more = __shfl(mine_upto, 63);
+        same = 0;
+        return kBins;
+    }
+    const int group = __builtin_ctzll(here);
+    const unsigned above = __shfl(from_top, group);
+    more = __shfl(mine_upto - before, group);
     __syncthreads();
-    unsigned room = (unsigned)p.keep;
-    find_bin(s, room);
-    const bool all = s.pick[0] == kBins;                  // every token that is there stays
-    const unsigned d1 = s.pick[0], count = s.pick[2];
-    unsigned T = 0;
-    if (!all) {
-        room -= s.pick[1];
-        const bool fits = count <= kList;
-        __syncthreads();
-        // ---- the tokens of that digit, tagged with the wavefront whose stretch they are in; those above it are counted
-        clear_hist(s);
-        __syncthreads();
-        unsigned mine = 0;
-        each(row, from, to, 256, [&](int, const unsigned(&k)[4]) {
+    // the group's bins, the highest first: thread t has bin t % 32 of stretches t / 32 and 32 + t / 32
+    const int bin = t % kGroup;
+    total = before = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const unsigned d = k[e] >> 21;
-                mine += d > d1;
-                const bool in = k[e] && d == d1;
-                if (in) atomicAdd(&s.hist[(k[e] >> 10 & (kBins - 1)) * kCopies + copy], 1u);
-                if (fits) {
-                    const unsigned long long who = __ballot(in);
-                    unsigned at = 0;
-                    if (who && lane == 0) at = atomicAdd(&s.listed, (unsigned)__popcll(who));
-                    at = __builtin_amdgcn_readfirstlane(at);
-                    at += __popcll(who & ~(~0ull << lane));
-                    if (in && at < kList) s.list[at] = (unsigned)wave << 21 | (k[e] & 0x1fffffu);
-                }
-            }
-        });
-        if (mine) atomicAdd(&s.above[wave], mine);
-        __syncthreads();
-        find_bin(s, room);
-        const unsigned d2 = s.pick[0];
-        room -= s.pick[1];
-        __syncthreads();
-        clear_hist(s);
-        __syncthreads();
-        const unsigned top = d1 << 11 | d2;               // the first 22 bits of T
-        if (fits) {
-            for (unsigned i = t; i < count; i += kSelect)
-                if ((s.list[i] >> 10 & (kBins - 1)) == d2) atomicAdd(&s.hist[(s.list[i] & 1023u) * kCopies + copy], 1u);
-        } else {
-            each(row, from, to, 256, [&](int, const unsigned(&k)[4]) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (k[e] && k[e] >> 10 == top) atomicAdd(&s.hist[(k[e] & 1023u) * kCopies + copy], 1u);
-            });
-        }
-        __syncthreads();
-        find_bin(s, room);
-        room -= s.pick[1];
-        T = top << 10 | s.pick[0];
-        // ---- how many tokens above T and equal to it each stretch has
-        if (fits) {
-            for (unsigned i = t; i < count; i += kSelect) {
-                const unsigned x = s.list[i], low = x & 0x1fffffu;
-                if (low > (T & 0x1fffffu)) atomicAdd(&s.above[x >> 21], 1u);
-                if (low == (T & 0x1fffffu)) atomicAdd(&s.equal[x >> 21], 1u);
-            }
-        } else {
-            unsigned more = 0, same = 0;
-            each(row, from, to, 256, [&](int, const unsigned(&k)[4]) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    more += k[e] > T && k[e] >> 21 == d1;
-                    same += k[e] == T;
-                }
-            });
-            if (more) atomicAdd(&s.above[wave], more);
-            if (same) atomicAdd(&s.equal[wave], same);
-        }
-    } else {
-        unsigned mine = 0;                                // T = 0: all keys are above it
-        each(row, from, to, 256, [&](int, const unsigned(&k)[4]) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mine += k[e] != 0u;
-        });
-        if (mine) atomicAdd(&s.above[wave], mine);
-        room = 0;
+    for (int q = t / kGroup; q < kMaxParts; q += kSelect / kGroup) {
+        if (q >= parts) break;
+        const unsigned v = hists[(size_t)q * kHist + (kGroups - 1 - group) * kGroup + kGroup - 1 - bin];
+        total += v;
+        before += q < part ? v : 0u;
+    }
+    total += __shfl_xor(total, 32);                       // a wavefront's two rows of bins
+    before += __shfl_xor(before, 32);
+    if (lane < kGroup) {
+        s.all[wave][lane] = total;
+        s.mine[wave][lane] = before;
     }
     __syncthreads();
+    total = before = 0;
+    if (lane < kGroup)
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            total += s.all[w][lane];
+            before += s.mine[w][lane];
+        }
+    const unsigned bin_upto = above + wave_prefix(total, lane), bin_top = bin_upto - total, mine_bin = wave_prefix(before, lane);
+    const int at = __builtin_ctzll(__ballot(bin_top <= room && room < bin_upto));
+    more += __shfl(mine_bin - before, at);
+    same = __shfl(before, at);
+    room -= __shfl(bin_top, at);
+    return (kGroups - 1 - group) * kGroup + kGroup - 1 - at;
+}
 
-    // ---- the list: behind the tokens of the stretches before, `taken` of them, `ties` equal to T
-    unsigned ties = 0, taken = 0;
+// The list of what stays: tokens above T and, of those equal to it, the first `room` of the row.  `taken` stay and `ties`
+// are equal to T in front of this workgroup's tokens (T = 0: all that are there stay, room = 0).
+__device__ __forceinline__ void list_kept(Shared &s, Stretch &x, const EvictParams &p, int g, int b, bool last, unsigned T, unsigned room,
+                                          unsigned taken, unsigned ties)
+{
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    int32_t *const ids = p.ids + ((size_t)b * p.Hkv + g) * (p.keep < p.N ? p.keep : p.N);
+    unsigned above = 0, equal = 0;
+    x.each([&](int, const unsigned(&k)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            above += __popcll(__ballot(k[e] > T));
+            if (room) equal += __popcll(__ballot(k[e] == T));              // (room > 0: T > 0, so only tokens that are there)
+        }
+    });
+    if (lane == 0) {
+        s.above[wave] = above;
+        s.equal[wave] = equal;
+    }
+    __syncthreads();
     for (int w = 0; w < wave; ++w) {
-        ties += s.equal[w];
         taken += s.above[w];
+        ties += s.equal[w];
     }
     taken += ties < room ? ties : room;
     const unsigned long long lower = ~(~0ull << lane);
-    each(row, from, to, 256, [&](int i, const unsigned(&k)[4]) {
+    x.each([&](int i, const unsigned(&k)[4]) {
         bool stays[4];
         unsigned long long eq[4], any = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             stays[e] = k[e] > T;
-            eq[e] = room ? __ballot(k[e] == T) : 0ull;    // (room > 0: T > 0, so no key that is not there)
+            eq[e] = room ? __ballot(k[e] == T) : 0ull;
             any |= eq[e];
         }
         if (any && ties < room) {
@@ -271,19 +306,96 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(const EvictParams
             }
         }
         unsigned at = taken;
-        unsigned long long st[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            st[e] = __ballot(stays[e]);
-            at += __popcll(st[e] & lower);
+            const unsigned long long st = __ballot(stays[e]);
+            at += __popcll(st & lower);
+            taken += __popcll(st);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 4; ++e)
             if (stays[e] && at < (unsigned)p.keep) ids[at++] = i + e;     // (weights that change meanwhile may be counted otherwise)
-            taken += __popcll(st[e]);
-        }
     });
-    if (g == 0 && wave == kWaves - 1 && lane == 0) p.dst_lens[b] = (int)(taken < (unsigned)p.keep ? taken : (unsigned)p.keep);
+    if (last && g == 0 && wave == kWaves - 1 && lane == 0) p.dst_lens[b] = (int)(taken < (unsigned)p.keep ? taken : (unsigned)p.keep);
+}
+
+// A row per workgroup: grid (KV heads, sequences).
+__global__ __launch_bounds__(kSelect) void evict_select_kernel(const EvictParams p)
+{
+    __shared__ __align__(16) Shared s;
+    const int g = blockIdx.x, b = blockIdx.y;
+    Stretch x;
+    x.open(p, g, b, 0, 1);
+    unsigned h[2], room = (unsigned)p.keep, T = 0;
+    count_digit<1>(s, x, 0);
+    own_bins(s, h);
+    const unsigned d1 = find_bin(s, h, room);
+    if (d1 == kBins) {
+        room = 0;
+    } else {
+        count_digit<2>(s, x, d1);
+        own_bins(s, h);
+        const unsigned d12 = d1 << 11 | find_bin(s, h, room);
+        count_digit<3>(s, x, d12);
+        own_bins(s, h);
+        T = d12 << 10 | find_bin(s, h, room);
+    }
+    list_kept(s, x, p, g, b, true, T, room, 0, 0);
+}
+
+// A stretch of a row per workgroup, grid (parts, KV heads, sequences): stage 1, 2, 3 count that digit of T, having found
+// the one before, stage 4 lists.
+//   p.hists   [stages 1 .. 3][rows][parts][kHist]: the bins, and behind them their sums by kGroup
+//   p.states  [rows][parts][3]: the digits found, the room left behind them, and of the stretches before the tokens above
+// Every workgroup of a row finds the same digits, each for itself.
+template <int STAGE>
+__global__ __launch_bounds__(kSelect) void evict_stage_kernel(const EvictParams p)
+{
+    __shared__ __align__(16) Shared s;
+    const int t = threadIdx.x, part = blockIdx.x, parts = gridDim.x, g = blockIdx.y, b = blockIdx.z;
+    const size_t row = (size_t)b * p.Hkv + g, rows = (size_t)p.B * p.Hkv;
+    unsigned *const hists = p.hists + row * parts * kHist;
+    unsigned *const state = p.states + (row * parts + part) * 3;
+    Stretch x;
+    x.open(p, g, b, part, parts);
+    unsigned found = 0, room = (unsigned)p.keep, taken = 0, ties = 0;
+    bool all = false;
+    if constexpr (STAGE > 1) {
+        if constexpr (STAGE > 2) {
+            found = state[0];
+            room = state[1];
+            taken = state[2];
+            all = found == ~0u;
+        }
+        if (!all) {
+            const unsigned *const in = hists + (STAGE - 2) * rows * parts * kHist;
+            unsigned more, same;                          // tokens above and in the bin in the stretches before this one
+            const unsigned d = find_bin_of_parts(s, in, part, parts, room, more, same);
+            all = d == kBins;
+            taken += more;
+            ties = STAGE == 4 ? same : 0;
+            found = all ? ~0u : found << (STAGE == 4 ? 10 : 11) | d;
+            if (STAGE < 4 && t == 0) {
+                state[0] = found;
+                state[1] = room;
+                state[2] = taken;
+            }
+        }
+    }
+    if constexpr (STAGE < 4) {
+        if (all) return;
+        count_digit<STAGE>(s, x, found);
+        unsigned h[2];
+        own_bins(s, h);
+        unsigned *const out = hists + ((STAGE - 1) * rows * parts + part) * kHist;
+        *reinterpret_cast<uint2 *>(out + (kBins - 2 - 2 * t)) = make_uint2(h[1], h[0]);
+        unsigned sum = h[0] + h[1];                       // 16 threads have a group's bins
+#pragma unroll
+        for (int o = 1; o < kGroup / 2; o <<= 1) sum += __shfl_xor(sum, o);
+        if (t % (kGroup / 2) == 0) out[kBins + kGroups - 1 - t / (kGroup / 2)] = sum;
+    } else {
+        list_kept(s, x, p, g, b, part == parts - 1, all ? 0u : found, all ? 0u : room, taken, ties);
+    }
 }
 
 template <int D>
@@ -311,9 +423,39 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p)
 
 } // namespace
 
+// Workgroups that share a row in the choice.
+int evict_parts(long long rows, long long N)
+{
+    if (N <= kHeld) return 1;
+    long long parts = (N + kPart - 1) / kPart;
+    if (rows * parts > 4 * num_cus()) parts = (N + kHeld - 1) / kHeld;     // the rows alone fill the chip
+    return (int)(parts < kMaxParts ? parts : kMaxParts);
+}
+
+size_t evict_hist_elems(long long rows, long long N)
+{
+    const int parts = evict_parts(rows, N);
+    return parts == 1 ? 0 : 3 * (size_t)rows * parts * kHist;
+}
+
+size_t evict_state_elems(long long rows, long long N)
+{
+    const int parts = evict_parts(rows, N);
+    return parts == 1 ? 0 : 3 * (size_t)rows * parts;
+}
+
 int launch_evict(const EvictParams &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)p.Hkv, (unsigned)p.B), dim3(kSelect), 0, stream, p);
+    const int parts = evict_parts((long long)p.B * p.Hkv, p.N);
+    if (parts == 1) {
+        hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)p.Hkv, (unsigned)p.B), dim3(kSelect), 0, stream, p);
+    } else {
+        const dim3 grid((unsigned)parts, (unsigned)p.Hkv, (unsigned)p.B);
+        hipLaunchKernelGGL(evict_stage_kernel<1>, grid, dim3(kSelect), 0, stream, p);
+        hipLaunchKernelGGL(evict_stage_kernel<2>, grid, dim3(kSelect), 0, stream, p);
+        hipLaunchKernelGGL(evict_stage_kernel<3>, grid, dim3(kSelect), 0, stream, p);
+        hipLaunchKernelGGL(evict_stage_kernel<4>, grid, dim3(kSelect), 0, stream, p);
+    }
     const int rows = 256 / (p.D / 8);
     const int most = p.keep < p.N ? p.keep : p.N;
     const dim3 grid((unsigned)((most + rows - 1) / rows), (unsigned)p.Hkv, (unsigned)p.B);

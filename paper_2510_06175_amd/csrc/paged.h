@@ -80,6 +80,7 @@ struct EvictParams {
     long long dst_w_cap;
     int32_t *kept;               // [B, Hkv, keep] or nullptr
     int32_t *ids;                // [B, Hkv, min(keep, N)] in the workspace: the kept tokens, for the move
+    unsigned *hists, *states;    // evict_hist_elems() and evict_state_elems() of the workspace (evict.hip)
 };
 
 __device__ __forceinline__ int clamped_len(const int32_t *lens, int b, int N)
@@ -97,6 +98,8 @@ int launch_rotary_table(const double *freqs, double base, int scaling, double fa
 int launch_rotary(const RotaryParams &p, int bf16, int D, bool append, hipStream_t stream);
 int launch_paged_attention(const PagedParams &p, int bf16, int D, hipStream_t stream);
 int launch_paged_weights(const PagedParams &p, hipStream_t stream);
+size_t evict_hist_elems(long long rows, long long N);
+size_t evict_state_elems(long long rows, long long N);
 int launch_evict(const EvictParams &p, hipStream_t stream);
 
 } // namespace vecinfer

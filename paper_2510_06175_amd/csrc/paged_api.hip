@@ -115,6 +115,19 @@ PagedLayout paged_layout(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t
     return w;
 }
 
+struct EvictLayout {
+    size_t off_hists, off_states, total;                  // the list of kept tokens comes first
+};
+
+EvictLayout evict_layout(int64_t rows, int64_t N, int64_t keep)
+{
+    EvictLayout w;
+    w.off_hists = up(sizeof(int32_t) * (size_t)rows * (keep < N ? keep : N));
+    w.off_states = w.off_hists + up(sizeof(unsigned) * evict_hist_elems(rows, N));
+    w.total = w.off_states + up(sizeof(unsigned) * evict_state_elems(rows, N));
+    return w;
+}
+
 int32_t paged_splits(const vecinfer_pages *p, int32_t B, int64_t N)
 {
     const int64_t groups = (int64_t)B * p->num_kv_heads;
@@ -282,7 +295,8 @@ int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const i
 size_t vecinfer_evict_workspace_bytes(int32_t num_kv_heads, int32_t B, int64_t N, int64_t keep)
 {
     if (num_kv_heads < 1 || B < 1 || N < 1 || N > kMaxTokens || keep < 1) return 0;
-    return up(sizeof(int32_t) * (size_t)B * num_kv_heads * (keep < N ? keep : N));
+    const EvictLayout w = evict_layout((int64_t)B * num_kv_heads, N, keep);
+    return w.total;
 }
 
 int vecinfer_paged_evict(const vecinfer_pages *src, const float *weights, int64_t w_cap, const int32_t *block_table,
@@ -328,7 +342,11 @@ int vecinfer_paged_evict(const vecinfer_pages *src, const float *weights, int64_
     p.dst_w = dst_weights;
     p.dst_w_cap = dst_w_cap;
     p.kept = kept;
-    p.ids = static_cast<int32_t *>(workspace);
+    const EvictLayout w = evict_layout((int64_t)B * p.Hkv, N, keep);
+    unsigned char *const ws = static_cast<unsigned char *>(workspace);
+    p.ids = reinterpret_cast<int32_t *>(ws);
+    p.hists = reinterpret_cast<unsigned *>(ws + w.off_hists);
+    p.states = reinterpret_cast<unsigned *>(ws + w.off_states);
     return launch_status(launch_evict(p, static_cast<hipStream_t>(stream)));
 }
 

@@ -102,6 +102,24 @@ def test_long(N, how):
     evict(c, weights(c, N, how), N // 3, 10, N // 6)
 
 
+@pytest.mark.parametrize("N,lens", [(16384, [16384, 16383, 1]), (16385, [16385, 0, 300]), (40000, [40000, 39999, 8191, 8193, 16384, 5])])
+@pytest.mark.parametrize("how", ["zero", "bits", "close"])
+def test_rows_of_one_or_more_workgroups(N, lens, how):
+    c = Cache(len(lens), 1, 64, 1024, N, seed=N)
+    evict(c, weights(c, N, how), 5000, 100, 1000, lens=lens)
+
+
+def test_very_long():
+    """More tokens than the registers of all workgroups of a row hold."""
+    c = Cache(1, 1, 64, 256, 1100003, fill=False)
+    evict(c, weights(c, 1100003), 1000, 3, 400)
+
+
+def test_many_long_rows():
+    c = Cache(24, 8, 64, 64, 20000, fill=False)
+    evict(c, weights(c, 20000, "ties"), 300, 3, 40, lens=[20000 - 700 * i for i in range(24)])
+
+
 def test_special_weights():
     """-0 equals 0, infinities are ordered, what is no number comes below them, and ties go to the lowest index."""
     c = Cache(1, 1, 64, 8, 12)
