@@ -530,7 +530,7 @@ size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q
  *              were.  With weights a second launch follows.
  *   workspace  as for vecinfer_decode_attention
  * Errors: EINVAL (null or misaligned pointers, sizes, strides, scale not finite, w_cap < N, weights_in alone),
- * EUNSUPPORTED (pages, G, B or H_kv above 65535, N > 2^30), EWORKSPACE, ELAUNCH.
+ * EUNSUPPORTED (pages, G, B or H_kv above 65535, N > 2^30, max_pages >= 2^31), EWORKSPACE, ELAUNCH.
  */
 int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const int64_t q_strides[2],
                              int32_t num_q_heads, const int32_t *block_table, int64_t max_pages,

@@ -108,7 +108,7 @@ PagedLayout paged_layout(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t
     w.off_o = take(sizeof(float) * (S > 1 ? rows * p->head_dim : 0));
     w.off_m = take(sizeof(float) * rows);
     w.off_l = take(sizeof(float) * rows);
-    w.off_words = take(sizeof(unsigned long long) * (size_t)B * p->num_kv_heads);
+    w.off_words = take(sizeof(unsigned long long) * kWordStep * (size_t)B * p->num_kv_heads);
     w.off_lse2 = take(weights ? sizeof(float) * (size_t)B * Hq : 0);
     w.off_scores = take(weights ? sizeof(float) * (size_t)B * Hq * ((N + 31) / 32 * 32) : 0);
     w.total = off;
@@ -128,14 +128,36 @@ EvictLayout evict_layout(int64_t rows, int64_t N, int64_t keep)
     return w;
 }
 
-int32_t paged_splits(const vecinfer_pages *p, int32_t B, int64_t N)
+// Splits of a sequence in vecinfer_paged_attention.  A compute unit holds one workgroup (8 wavefronts of 150 registers),
+// and two rounds of them are slower than one where all sequences are alike: a workgroup's start and end take 7 us (one
+// sequence of 196608 tokens, 8 KV heads: 126 us in 32 splits, 141 in 48, 136 in 64).  So as many as fill the chip once, and
+//   - no more than pay for themselves: the merge takes 0.15 us per split (with up to four query heads per KV head, in
+//     proportion with more), a workgroup 10 ns per token, which together are least at sqrt(N / 14) splits (1000 tokens: 8.5
+//     us in 4, 7.8 in 8, 8.0 in 16, 9.7 in 32; 4000: 12.8 in 8, 10.5 in 16, 11.7 in 32; 8 / 1 heads, 8000: 20.0 in 8, 16.8
+//     in 16, 18.4 in 32);
+//   - whole up to 256 tokens, one round of a workgroup's wavefronts (200 tokens 5.6 us whole, 6.7 to 7.0 in splits);
+//   - more where sequences differ in length (seq_lens are given) and are long, 4000 tokens per split and up, or where one
+//     round would leave an eighth of the chip idle: then short workgroups make room for others (N / 8 to N tokens, 8 KV
+//     heads: 32 sequences, 8000 tokens 109.5 us whole, 101.6 in four; 16, 16000 113 in two, 100 in four; 8, 30000 109 in four,
+//     96 in eight; but 32, 2000 31.8 whole, 40.8 in four; 8, 8000 35.3 in four, 34.8 in eight.  32 of 8192 tokens each, 163
+//     whole and 172 in four, pay for that where they come with seq_lens).
+int32_t paged_splits(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t N, bool ragged)
 {
-    const int64_t groups = (int64_t)B * p->num_kv_heads;
-    int64_t s = 2 * num_cus() / groups;
-    const int64_t cap = (N + 127) / 128;
-    if (s > cap) s = cap;
+    const int64_t groups = (int64_t)B * p->num_kv_heads, G = Hq / p->num_kv_heads;
+    int64_t s = num_cus() / groups;
+    if (s < 1) s = 1;
+    if (N >= 4000 * s && ((ragged && B > 1) || 8 * s * groups < 7 * num_cus())) s = 2 * s > 4 ? 2 * s : 4;
+    const int64_t worth = (int64_t)sqrt((double)N / (3.5 * (double)(G > 4 ? G : 4)));
+    if (s > worth) s = worth;
     if (s > VECINFER_MAX_SPLITS) s = VECINFER_MAX_SPLITS;
-    return s < 1 ? 1 : (int32_t)s;
+    return s < 1 || N <= 256 ? 1 : (int32_t)s;
+}
+
+// The most of them, for batches of any lengths.
+int32_t most_splits(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t N)
+{
+    const int32_t a = paged_splits(p, Hq, B, N, false), b = paged_splits(p, Hq, B, N, true);
+    return a > b ? a : b;
 }
 
 } // namespace
@@ -230,7 +252,7 @@ size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q
 {
     if (pages_ok(pages) != VECINFER_OK || num_q_heads < 1 || num_q_heads % pages->num_kv_heads) return 0;
     if (B < 1 || N < 1 || N > kMaxTokens || num_splits < 0 || num_splits > VECINFER_MAX_SPLITS) return 0;
-    return paged_layout(pages, num_q_heads, B, N, num_splits ? num_splits : paged_splits(pages, B, N), weights != 0).total;
+    return paged_layout(pages, num_q_heads, B, N, num_splits ? num_splits : most_splits(pages, num_q_heads, B, N), weights != 0).total;
 }
 
 int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const int64_t q_strides[2], int32_t num_q_heads,
@@ -249,9 +271,9 @@ int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const i
         return VECINFER_EINVAL;
     if ((weights_in && !weights_out) || (weights_out && w_cap < N)) return VECINFER_EINVAL;
     const int G = num_q_heads / pages->num_kv_heads;
-    if (G > 16 || B > 65535 || N > kMaxTokens) return VECINFER_EUNSUPPORTED;
+    if (G > 16 || B > 65535 || N > kMaxTokens || max_pages > 0x7fffffffLL) return VECINFER_EUNSUPPORTED;
 
-    int32_t S = num_splits ? num_splits : paged_splits(pages, B, N);
+    int32_t S = num_splits ? num_splits : paged_splits(pages, num_q_heads, B, N, seq_lens != nullptr);
     PagedLayout w = paged_layout(pages, num_q_heads, B, N, S, weights_out != nullptr);
     if (num_splits == 0)                // fewer where the workspace has no room for that many
         while (S > 1 && workspace_bytes < w.total) w = paged_layout(pages, num_q_heads, B, N, --S, weights_out != nullptr);

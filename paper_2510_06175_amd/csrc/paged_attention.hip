@@ -60,13 +60,15 @@ __device__ __forceinline__ typename Vec<E>::v8 as_vec(unsigned a, unsigned b, un
 }
 
 // Called by all threads of a workgroup whose partials are stored: the last of the S workgroups of this (sequence, KV
-// head) writes the output rows (split_merge.h).
+// head) writes the output rows (split_merge.h).  The rows of the first kBatch splits travel while the weights are
+// worked out, a wavefront per head.
 template <typename E, int D, int KG, int NW>
 __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, size_t bg, size_t row0)
 {
-    constexpr int kBlock = NW * 64, kBatch = 16;
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), S = p.S, G = p.G;
-    arrival_t *const word = p.words + bg;
+    constexpr int kBlock = NW * 64, kElems = (KG * D + kBlock - 1) / kBlock, kBatch = 32 / kElems;
+    static_assert(kBatch >= 4, "elements of a thread");
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), S = p.S, G = p.G, GD = G * D;
+    arrival_t *const word = p.words + bg * kWordStep;
     unsigned *const flag = reinterpret_cast<unsigned *>(lds);
     float *const wt_s = lds + 4, *const den_s = wt_s + KG * kMergeSplits;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's stores are acknowledged
@@ -77,6 +79,20 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, siz
     }
     __syncthreads();
     if (*flag == 0u) return;                              // (the same for the whole workgroup)
+    const float *const po = p.part_o + bg * S * GD;
+    float v[kElems][kBatch];
+    auto request = [&](int s0) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (s0 + j >= S) break;
+#pragma unroll
+            for (int i = 0; i < kElems; ++i) {
+                const int e = t + i * kBlock;
+                v[i][j] = e < GD ? shared_load(po + (size_t)(s0 + j) * GD + e) : 0.f;
+            }
+        }
+    };
+    request(0);
     if (t == 0) __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     for (int h = wave; h < G; h += NW) {
         const float *const pm = p.part_m + bg * S * G + h, *const pl = p.part_l + bg * S * G + h;
@@ -86,9 +102,10 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, siz
             const int s = lane + 64 * i;
             m[i] = s < S ? shared_load(pm + (size_t)s * G) : -INFINITY;
             l[i] = s < S ? shared_load(pl + (size_t)s * G) : 0.f;
-            M = fmaxf(M, m[i]);
         }
-        M = wave_max(M);
+#pragma unroll
+        for (int i = 0; i < kMergeSplits / 64; ++i) M = fmaxf(M, m[i]);
+        M = wave_all(M, [](float a, float b) { return fmaxf(a, b); });
         const float at = M > -INFINITY ? M : 0.f;         // nothing to attend to: all weights 0
 #pragma unroll
         for (int i = 0; i < kMergeSplits / 64; ++i) {
@@ -96,7 +113,7 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, siz
             wt_s[h * kMergeSplits + lane + 64 * i] = w;
             den = fmaf(w, l[i], den);
         }
-        den = wave_sum(den);
+        den = wave_all(den, [](float a, float b) { return a + b; });
         if (lane == 0) {
             const float total = den == 0.f ? -INFINITY : M + log2f(den);
             den_s[h] = den;
@@ -105,60 +122,74 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, siz
         }
     }
     __syncthreads();
-    const float *const po = p.part_o + bg * S * G * D;
-    E *const out = static_cast<E *>(p.out) + row0 * D;
-    for (int e = t; e < G * D; e += kBlock) {
-        const int h = e / D;
-        float acc = 0.f;
-        for (int s0 = 0; s0 < S; s0 += kBatch) {
-            float v[kBatch];
+    float acc[kElems];
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j) v[j] = shared_load(po + (size_t)(s0 + j < S ? s0 + j : S - 1) * G * D + e);
+    for (int i = 0; i < kElems; ++i) acc[i] = 0.f;
+    for (int s0 = 0;;) {
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j)              // (behind the last split the weights are 0: m = -inf)
-                if (s0 + j < S) acc = fmaf(wt_s[h * kMergeSplits + s0 + j], v[j], acc);
+        for (int j = 0; j < kBatch; ++j) {
+            if (s0 + j >= S) break;
+#pragma unroll
+            for (int i = 0; i < kElems; ++i) {
+                const int e = t + i * kBlock;
+                if (e < GD) acc[i] = fmaf(wt_s[e / D * kMergeSplits + s0 + j], v[i][j], acc[i]);
+            }
         }
-        const float den = den_s[h];
-        out[e] = (E)(den == 0.f ? 0.f : acc / den);
+        s0 += kBatch;
+        if (s0 >= S) break;
+        request(s0);
+    }
+    E *const out = static_cast<E *>(p.out) + row0 * D;
+#pragma unroll
+    for (int i = 0; i < kElems; ++i) {
+        const int e = t + i * kBlock;
+        if (e >= GD) continue;
+        const float den = den_s[e / D];
+        out[e] = (E)(den == 0.f ? 0.f : acc[i] / den);
     }
 }
 
+// (what the first requests need comes first: the command processor puts the leading arguments into registers)
 template <typename E, int D, int KG, int NW, bool SCORES>
-__global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedParams p)
+__global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t *seq_lens, const int32_t *block_table, const char *q,
+                                                                  const char *k_pool, const char *v_pool, int N, int max_pages, int G,
+                                                                  int S, const PagedParams p)
 {
     constexpr int kSteps = D / 32;                        // matrix instructions per sub-tile of keys
     constexpr int kVE = D / 16;                           // channels of a value row that a lane loads
     constexpr int kVW = kVE / 2;                          // .. in 32-bit words
     typedef typename Vec<E>::v8 vec8;
+    typedef unsigned words __attribute__((ext_vector_type(kVW)));
     constexpr int kJoin = NW * KG * (D + 2), kMerge = 4 + KG * (kMergeSplits + 1);
     __shared__ __align__(16) float lds[kJoin > kMerge ? kJoin : kMerge];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int kg = lane >> 4, c = lane & 15, G = p.G;
+    const int kg = lane >> 4, c = lane & 15;
     const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
     const size_t bg = (size_t)b * p.Hkv + g, row0 = (size_t)b * p.Hq + (size_t)g * G;
     arrival_t seen = 0;
-    if (p.S > 1 && t == 0) seen = arrival_peek(p.words + bg);
+    if (S > 1 && t == 0) seen = arrival_peek(p.words + bg * kWordStep);
 
-    const int len = clamped_len(p.seq_lens, b, p.N);
-    int chunk = (int)(((long long)len + p.S - 1) / p.S);
+    const int len = clamped_len(seq_lens, b, N);
+    int chunk = (int)(((long long)len + S - 1) / S);
     chunk = (chunk + kTokens - 1) / kTokens * kTokens;
     const long long first = (long long)split * chunk;
     const int n0 = (int)(first < len ? first : len), n1 = (int)(first + chunk < len ? first + chunk : len);
 
     vec8 qf[kSteps];
     {
-        const char *const row = p.q + b * p.q_b + (long long)(g * G + (c < G ? c : 0)) * p.q_h;
+        const unsigned head = c < G ? ~0u : 0u;            // spare columns: zeros (by a mask: the request is not to wait for a branch)
+        const char *const row = q + b * p.q_b + (long long)(g * G + (c < G ? c : 0)) * p.q_h;
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
             const uint4 x = reinterpret_cast<const uint4 *>(row)[4 * j + kg];
-            qf[j] = c < G ? __builtin_bit_cast(vec8, x) : as_vec<E>(0, 0, 0, 0);
+            qf[j] = as_vec<E>(x.x & head, x.y & head, x.z & head, x.w & head);
         }
     }
 
-    const int32_t *const pages = p.block_table + b * p.max_pages;
-    const int shift = p.pages.shift, last_col = (p.N - 1) >> shift;
+    const int32_t *const pages = block_table + (size_t)b * max_pages;
+    const int shift = p.pages.shift, last_col = (N - 1) >> shift;
     const unsigned slot_mask = (1u << shift) - 1;
-    const char *const k0 = p.pages.k + (size_t)g * p.pages.k_head, *const v0 = p.pages.v + (size_t)g * p.pages.v_head;
+    const char *const k0 = k_pool + (size_t)g * p.pages.k_head, *const v0 = v_pool + (size_t)g * p.pages.v_head;
     const int krow = 8 * (c >> 2) + (c & 3);              // this lane's key token of sub-tile 0; of sub-tile 1: + 4
     auto page_at = [&](int tok) {
         const int col = tok >> shift;
@@ -170,48 +201,48 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedPar
 #pragma unroll
     for (int i = 0; i < kVE; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
+    // Keys and values of the next tile are requested as soon as this one's have been used, its pages a tile before that
+    // (196608 tokens, 32 / 8 heads: 142 us with all requests at the tile's start, 139 so).  Values are not to be kept in any
+    // cache: 125.  Keys are: a request takes 64 bytes of each row, half a cache line, and the next one the other half (without
+    // caching 129 us, and a workgroup by itself a quarter slower).
+    uint4 kr[2][kSteps];
+    unsigned vr[8][kVW];
+    auto load_k = [&](int t0, unsigned page) {
+        const char *row = k0 + (size_t)(page < p.pages.num_pages ? page : 0u) * p.pages.k_page +
+                          (size_t)((unsigned)(t0 + krow) & slot_mask) * p.pages.k_slot + 16 * kg;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) kr[u][j] = *reinterpret_cast<const uint4 *>(row + 64 * j);
+            row += 4 * (size_t)p.pages.k_slot;
+        }
+    };
+    auto load_v = [&](int t0, unsigned page) {
+        const char *row = v0 + (size_t)(page < p.pages.num_pages ? page : 0u) * p.pages.v_page +
+                          (size_t)((unsigned)(t0 + 8 * kg) & slot_mask) * p.pages.v_slot + 2 * kVE * c;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const words x = __builtin_nontemporal_load(reinterpret_cast<const words *>(row));
+#pragma unroll
+            for (int w = 0; w < kVW; ++w) vr[j][w] = x[w];
+            row += p.pages.v_slot;
+        }
+    };
     int t0 = n0 + wave * kTokens;
-    int next_k = 0, next_v = 0;
+    unsigned page_k = 0, page_v = 0;                      // of the tile in hand, then of the next
     if (t0 < n1) {
-        next_k = page_at(t0 + krow);
-        next_v = page_at(t0 + 8 * kg);
+        page_k = (unsigned)page_at(t0 + krow);
+        page_v = (unsigned)page_at(t0 + 8 * kg);
+        load_k(t0, page_k);
+        load_v(t0, page_v);
     }
-    for (; t0 < n1; t0 += NW * kTokens) {
-        const unsigned page_k = (unsigned)next_k, page_v = (unsigned)next_v;
+    while (t0 < n1) {
         const bool there = page_v < p.pages.num_pages;
-        uint4 kr[2][kSteps];
-        unsigned vr[8][kVW];
-        {
-            const char *row = k0 + (size_t)(page_k < p.pages.num_pages ? page_k : 0u) * p.pages.k_page +
-                              (size_t)((unsigned)(t0 + krow) & slot_mask) * p.pages.k_slot + 16 * kg;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-#pragma unroll
-                for (int j = 0; j < kSteps; ++j) kr[u][j] = *reinterpret_cast<const uint4 *>(row + 64 * j);
-                row += 4 * (size_t)p.pages.k_slot;
-            }
-        }
-        {
-            const char *row = v0 + (size_t)(there ? page_v : 0u) * p.pages.v_page +
-                              (size_t)((unsigned)(t0 + 8 * kg) & slot_mask) * p.pages.v_slot + 2 * kVE * c;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if constexpr (kVW == 4) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(row);
-                    vr[j][0] = x.x; vr[j][1] = x.y; vr[j][2] = x.z; vr[j][3] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2 *>(row);
-                    vr[j][0] = x.x; vr[j][1] = x.y;
-                }
-                row += p.pages.v_slot;
-            }
-        }
         const int tn = t0 + NW * kTokens;
         if (tn < n1) {
-            next_k = page_at(tn + krow);
-            next_v = page_at(tn + 8 * kg);
+            page_k = (unsigned)page_at(tn + krow);
+            page_v = (unsigned)page_at(tn + 8 * kg);
         }
-
         // ---- scores, in log2 units: head c, tokens t0 + 8 kg + e
         float s[8];
 #pragma unroll
@@ -222,6 +253,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedPar
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[4 * u + r] = d[r] * p.scale2;
         }
+        if (tn < n1) load_k(tn, page_k);
         // A tile with a hole, or the sequence's last: what is not there has no score, and whatever its rows hold (an
         // infinity times a probability of 0 is NaN) is taken out.
         if (t0 + kTokens > n1 || !__all(there)) {
@@ -273,6 +305,8 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedPar
             acc[i] = Vec<E>::mfma(a, hi, acc[i]);
             acc[i] = Vec<E>::mfma(a, lo, acc[i]);
         }
+        if (tn < n1) load_v(tn, page_v);
+        t0 = tn;
     }
 
     // ---- the wavefronts join
@@ -304,7 +338,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedPar
             den = fmaf(f, l_s[w * KG + h], den);
             o = fmaf(f, o_s[(w * KG + h) * D + ch], o);
         }
-        if (p.S == 1) {
+        if (S == 1) {
             static_cast<E *>(p.out)[(row0 + h) * D + ch] = (E)(den == 0.f ? 0.f : o / den);
             if (ch == 0) {
                 const float total = den == 0.f ? -INFINITY : M - Vec<E>::kLift + log2f(den);
@@ -312,7 +346,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedPar
                 if (p.lse2) p.lse2[row0 + h] = total;
             }
         } else {
-            const size_t at_s = (bg * p.S + split) * G + h;
+            const size_t at_s = (bg * S + split) * G + h;
             shared_store(p.part_o + at_s * D + ch, o);
             if (ch == 0) {
                 shared_store(p.part_m + at_s, M - Vec<E>::kLift);
@@ -320,8 +354,8 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const PagedPar
             }
         }
     }
-    if (p.S == 1) return;
-    if (t == 0) arrival_open(p.words + bg, seen, p.nonce);
+    if (S == 1) return;
+    if (t == 0) arrival_open(p.words + bg * kWordStep, seen, p.nonce);
     merge_last<E, D, KG, NW>(p, lds, bg, row0);
 }
 
@@ -356,7 +390,7 @@ void start(const PagedParams &p, hipStream_t stream)
 {
     constexpr int NW = 8;
     const dim3 grid((unsigned)p.S, (unsigned)p.Hkv, (unsigned)p.B), block(NW * 64);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p.seq_lens, p.block_table, p.q, p.pages.k, p.pages.v, p.N, (int)p.max_pages, p.G, p.S, p); };
     if (p.scores)
         p.G <= 4 ? go(paged_attention_kernel<E, D, 4, NW, true>) : go(paged_attention_kernel<E, D, 16, NW, true>);
     else
