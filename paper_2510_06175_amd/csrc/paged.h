@@ -44,7 +44,7 @@ struct RotaryParams {
 };
 
 // Arrival words lie 256 bytes apart: the atomics of all workgroups on neighbouring words would queue for one cache line
-// (1000 tokens, 8 KV heads in 32 splits: 14.6 us so, PLACEHOLDER apart).
+// (1000 tokens, 8 KV heads in 32 splits: 14.6 us so, 9.7 apart).
 constexpr int kWordStep = 32;
 
 struct PagedParams {
@@ -54,10 +54,12 @@ struct PagedParams {
     const int32_t *block_table;  // [B, max_pages]
     long long max_pages;
     const int32_t *seq_lens;     // [B] or nullptr: N
-    int B, Hq, Hkv, G, N, S;
+    int B, Hq, Hkv, G, N;
+    int S;                       // splits of every sequence; or with `least` workgroups per KV head
+    int least;                   // 0, or: splits in proportion to the lengths, of at least this many tiles; 2 <= B <= 64, B < S
     float scale2;                // softmax scale * log2(e)
-    float *part_o;               // [B, Hkv, S, G, D]  partials, as in DecodeParams
-    float *part_m, *part_l;      // [B, Hkv, S, G]
+    float *part_o;               // [B, Hkv, S, G, D]  partials, as in DecodeParams; with `least` [Hkv, S, G, D]
+    float *part_m, *part_l;      // [B, Hkv, S, G]     or [Hkv, S, G]
     unsigned long long *words;   // [B, Hkv, kWordStep]: an arrival word (split_merge.h) each, and nothing else in its cache lines
     unsigned long long nonce;
     void *out;                   // [B, Hq, D]
@@ -87,13 +89,15 @@ struct EvictParams {
     unsigned *hists, *states;    // evict_hist_elems() and evict_state_elems() of the workspace (evict.hip)
 };
 
+__device__ __forceinline__ int clamped_lane(int v, int N) { return v < 0 ? 0 : (v > N ? N : v); }
+
 __device__ __forceinline__ int clamped_len(const int32_t *lens, int b, int N)
 {
     if (!lens) return N;
     // b is the same for the whole workgroup: a scalar load, which does not queue behind vector loads
     typedef const int32_t __attribute__((address_space(4))) *const_i32_ptr;
     const int v = ((const_i32_ptr)(uintptr_t)lens)[b];
-    return v < 0 ? 0 : (v > N ? N : v);
+    return clamped_lane(v, N);
 }
 
 // log2 of the sum, and the sum itself, go to natural units in one place

@@ -95,9 +95,10 @@ struct PagedLayout {
     size_t off_o, off_m, off_l, off_words, off_lse2, off_scores, total;
 };
 
-PagedLayout paged_layout(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t N, int32_t S, bool weights)
+// parts: partials of a (split, KV head) each
+PagedLayout paged_layout(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t N, int64_t parts, bool weights)
 {
-    const size_t rows = (size_t)B * Hq * S;
+    const size_t rows = (size_t)parts * (Hq / p->num_kv_heads);
     PagedLayout w;
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -105,7 +106,7 @@ PagedLayout paged_layout(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t
         off += up(bytes);
         return at;
     };
-    w.off_o = take(sizeof(float) * (S > 1 ? rows * p->head_dim : 0));
+    w.off_o = take(sizeof(float) * rows * p->head_dim);
     w.off_m = take(sizeof(float) * rows);
     w.off_l = take(sizeof(float) * rows);
     w.off_words = take(sizeof(unsigned long long) * kWordStep * (size_t)B * p->num_kv_heads);
@@ -128,36 +129,53 @@ EvictLayout evict_layout(int64_t rows, int64_t N, int64_t keep)
     return w;
 }
 
-// Splits of a sequence in vecinfer_paged_attention.  A compute unit holds one workgroup (8 wavefronts of 150 registers),
-// and two rounds of them are slower than one where all sequences are alike: a workgroup's start and end take 7 us (one
-// sequence of 196608 tokens, 8 KV heads: 126 us in 32 splits, 141 in 48, 136 in 64).  So as many as fill the chip once, and
+// How the tokens of a batch are dealt to workgroups: `splits` of every sequence; or, with `least`, `splits` workgroups
+// per KV head, dealt by the sequences' lengths (PagedParams).
+struct Cut {
+    int32_t splits, least;
+    int64_t parts(const vecinfer_pages *p, int32_t B) const
+    {
+        return least ? (int64_t)p->num_kv_heads * splits : (splits > 1 ? (int64_t)B * p->num_kv_heads * splits : 0);
+    }
+};
+
+constexpr int32_t kDealt = 64;           // most sequences of a batch that is dealt by length: a lane each
+
+// A compute unit holds one workgroup (8 wavefronts of 150 registers), and two rounds of them are slower than one where all
+// are alike: a workgroup's start and end take 7 us (one sequence of 196608 tokens, 8 KV heads: 126 us in 32 splits, 141 in
+// 48, 136 in 64).  So as many as fill the chip once, and
 //   - no more than pay for themselves: the merge takes 0.15 us per split (with up to four query heads per KV head, in
 //     proportion with more), a workgroup 10 ns per token, which together are least at sqrt(N / 14) splits (1000 tokens: 8.5
 //     us in 4, 7.8 in 8, 8.0 in 16, 9.7 in 32; 4000: 12.8 in 8, 10.5 in 16, 11.7 in 32; 8 / 1 heads, 8000: 20.0 in 8, 16.8
 //     in 16, 18.4 in 32);
 //   - whole up to 256 tokens, one round of a workgroup's wavefronts (200 tokens 5.6 us whole, 6.7 to 7.0 in splits);
-//   - more where sequences differ in length (seq_lens are given) and are long, 4000 tokens per split and up, or where one
-//     round would leave an eighth of the chip idle: then short workgroups make room for others (N / 8 to N tokens, 8 KV
-//     heads: 32 sequences, 8000 tokens 109.5 us whole, 101.6 in four; 16, 16000 113 in two, 100 in four; 8, 30000 109 in four,
-//     96 in eight; but 32, 2000 31.8 whole, 40.8 in four; 8, 8000 35.3 in four, 34.8 in eight.  32 of 8192 tokens each, 163
-//     whole and 172 in four, pay for that where they come with seq_lens).
-int32_t paged_splits(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t N, bool ragged)
+//   - more where one round would leave an eighth of the chip idle and splits are long (4000 tokens).
+// Sequences that come with lengths of their own, 4000 tokens and up, are dealt by length to one round of workgroups, or,
+// where there are more than a quarter as many as compute units per KV head, to so many rounds that each has one and there is
+// one round more (N / 8 to N tokens, in the same splits / dealt: 8 KV heads, 4 x 30000 62.3 / 54.8 us, 8 x 8000 35.6 /
+// 32.4, 16 x 8000 60.0 / 56.7, 64 x 6000 162 / 159; 4 KV heads, 9 x 30000 69.0 / 58.5; 32 x 8192 102 to 112, depending on which
+// come first, / 104, and 32 of 8192 each 163 whole, 168 dealt.  Shorter ones not: 32 x 2000 31.7 / 35, 4 x 1000 8.6 / 8.9).
+Cut even_cut(const vecinfer_pages *p, int32_t B, int64_t N, int64_t worth)
 {
-    const int64_t groups = (int64_t)B * p->num_kv_heads, G = Hq / p->num_kv_heads;
+    const int64_t groups = (int64_t)B * p->num_kv_heads;
     int64_t s = num_cus() / groups;
     if (s < 1) s = 1;
-    if (N >= 4000 * s && ((ragged && B > 1) || 8 * s * groups < 7 * num_cus())) s = 2 * s > 4 ? 2 * s : 4;
-    const int64_t worth = (int64_t)sqrt((double)N / (3.5 * (double)(G > 4 ? G : 4)));
+    if (N >= 4000 * s && groups <= num_cus() && 8 * s * groups < 7 * num_cus()) s = 2 * s > 4 ? 2 * s : 4;
     if (s > worth) s = worth;
     if (s > VECINFER_MAX_SPLITS) s = VECINFER_MAX_SPLITS;
-    return s < 1 || N <= 256 ? 1 : (int32_t)s;
+    return {s < 1 || N <= 256 ? 1 : (int32_t)s, 0};
 }
 
-// The most of them, for batches of any lengths.
-int32_t most_splits(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t N)
+Cut auto_cut(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t N, bool lengths)
 {
-    const int32_t a = paged_splits(p, Hq, B, N, false), b = paged_splits(p, Hq, B, N, true);
-    return a > b ? a : b;
+    const int64_t G = Hq / p->num_kv_heads;
+    const int64_t worth = (int64_t)sqrt((double)N / (3.5 * (double)(G > 4 ? G : 4)));
+    if (!lengths || B < 2 || B > kDealt || N < 4000) return even_cut(p, B, N, worth);
+    int64_t per_head = num_cus() / p->num_kv_heads;
+    if (per_head < 1) per_head = 1;
+    int64_t slots = per_head >= 4 * B ? per_head : (B + 2 * per_head - 1) / per_head * per_head;
+    if (slots > VECINFER_MAX_SPLITS) slots = VECINFER_MAX_SPLITS;
+    return {(int32_t)slots, (int32_t)((N + 32 * worth - 1) / (32 * worth))};
 }
 
 } // namespace
@@ -252,7 +270,9 @@ size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q
 {
     if (pages_ok(pages) != VECINFER_OK || num_q_heads < 1 || num_q_heads % pages->num_kv_heads) return 0;
     if (B < 1 || N < 1 || N > kMaxTokens || num_splits < 0 || num_splits > VECINFER_MAX_SPLITS) return 0;
-    return paged_layout(pages, num_q_heads, B, N, num_splits ? num_splits : most_splits(pages, num_q_heads, B, N), weights != 0).total;
+    const Cut fixed{num_splits, 0}, even = auto_cut(pages, num_q_heads, B, N, false), dealt = auto_cut(pages, num_q_heads, B, N, true);
+    const int64_t a = even.parts(pages, B), b = dealt.parts(pages, B);
+    return paged_layout(pages, num_q_heads, B, N, num_splits ? fixed.parts(pages, B) : (a > b ? a : b), weights != 0).total;
 }
 
 int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const int64_t q_strides[2], int32_t num_q_heads,
@@ -273,10 +293,16 @@ int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const i
     const int G = num_q_heads / pages->num_kv_heads;
     if (G > 16 || B > 65535 || N > kMaxTokens || max_pages > 0x7fffffffLL) return VECINFER_EUNSUPPORTED;
 
-    int32_t S = num_splits ? num_splits : paged_splits(pages, num_q_heads, B, N, seq_lens != nullptr);
-    PagedLayout w = paged_layout(pages, num_q_heads, B, N, S, weights_out != nullptr);
-    if (num_splits == 0)                // fewer where the workspace has no room for that many
-        while (S > 1 && workspace_bytes < w.total) w = paged_layout(pages, num_q_heads, B, N, --S, weights_out != nullptr);
+    Cut cut{num_splits, 0};
+    if (num_splits == 0) cut = auto_cut(pages, num_q_heads, B, N, seq_lens != nullptr);
+    PagedLayout w = paged_layout(pages, num_q_heads, B, N, cut.parts(pages, B), weights_out != nullptr);
+    if (num_splits == 0 && workspace_bytes < w.total) {     // fewer where the workspace has no room for that many
+        if (cut.least) cut = auto_cut(pages, num_q_heads, B, N, false);
+        for (;; --cut.splits) {
+            w = paged_layout(pages, num_q_heads, B, N, cut.parts(pages, B), weights_out != nullptr);
+            if (cut.splits == 1 || workspace_bytes >= w.total) break;
+        }
+    }
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < w.total) return VECINFER_EWORKSPACE;
     unsigned char *const ws = static_cast<unsigned char *>(workspace);
     PagedParams p = {};
@@ -292,13 +318,14 @@ int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const i
     p.Hkv = pages->num_kv_heads;
     p.G = G;
     p.N = (int)N;
-    p.S = S;
+    p.S = cut.splits;
+    p.least = cut.least;
     p.scale2 = scale * kLog2e;
     p.part_o = reinterpret_cast<float *>(ws + w.off_o);
     p.part_m = reinterpret_cast<float *>(ws + w.off_m);
     p.part_l = reinterpret_cast<float *>(ws + w.off_l);
     p.words = reinterpret_cast<unsigned long long *>(ws + w.off_words);
-    p.nonce = S > 1 ? next_nonce() : 0;
+    p.nonce = cut.splits > 1 ? next_nonce() : 0;
     p.out = out;
     p.lse = lse;
     if (weights_out) {

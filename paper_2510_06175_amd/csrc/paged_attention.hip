@@ -22,6 +22,8 @@
 #include "paged.h"
 #include "split_merge.h"
 
+#include <type_traits>
+
 namespace vecinfer {
 
 namespace {
@@ -59,16 +61,26 @@ __device__ __forceinline__ typename Vec<E>::v8 as_vec(unsigned a, unsigned b, un
     return __builtin_bit_cast(typename Vec<E>::v8, u);
 }
 
+// Sum over the lanes up to this one.
+__device__ __forceinline__ unsigned wave_upto(unsigned v, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned x = __shfl_up(v, o);
+        if (lane >= o) v += x;
+    }
+    return v;
+}
+
 // Called by all threads of a workgroup whose partials are stored: the last of the S workgroups of this (sequence, KV
 // head) writes the output rows (split_merge.h).  The rows of the first kBatch splits travel while the weights are
 // worked out, a wavefront per head.
 template <typename E, int D, int KG, int NW>
-__device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, size_t bg, size_t row0)
+__device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, arrival_t *word, size_t first, int S, size_t row0)
 {
     constexpr int kBlock = NW * 64, kElems = (KG * D + kBlock - 1) / kBlock, kBatch = 32 / kElems;
     static_assert(kBatch >= 4, "elements of a thread");
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), S = p.S, G = p.G, GD = G * D;
-    arrival_t *const word = p.words + bg * kWordStep;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), G = p.G, GD = G * D;
     unsigned *const flag = reinterpret_cast<unsigned *>(lds);
     float *const wt_s = lds + 4, *const den_s = wt_s + KG * kMergeSplits;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's stores are acknowledged
@@ -79,7 +91,7 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, siz
     }
     __syncthreads();
     if (*flag == 0u) return;                              // (the same for the whole workgroup)
-    const float *const po = p.part_o + bg * S * GD;
+    const float *const po = p.part_o + first * GD;
     float v[kElems][kBatch];
     auto request = [&](int s0) {
 #pragma unroll
@@ -95,7 +107,7 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, siz
     request(0);
     if (t == 0) __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     for (int h = wave; h < G; h += NW) {
-        const float *const pm = p.part_m + bg * S * G + h, *const pl = p.part_l + bg * S * G + h;
+        const float *const pm = p.part_m + first * G + h, *const pl = p.part_l + first * G + h;
         float m[kMergeSplits / 64], l[kMergeSplits / 64], M = -INFINITY, den = 0.f;
 #pragma unroll
         for (int i = 0; i < kMergeSplits / 64; ++i) {
@@ -150,10 +162,10 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, siz
 }
 
 // (what the first requests need comes first: the command processor puts the leading arguments into registers)
-template <typename E, int D, int KG, int NW, bool SCORES>
+template <typename E, int D, int KG, int NW, bool SCORES, bool DEALT>
 __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t *seq_lens, const int32_t *block_table, const char *q,
                                                                   const char *k_pool, const char *v_pool, int N, int max_pages, int G,
-                                                                  int S, const PagedParams p)
+                                                                  int least, const PagedParams p)
 {
     constexpr int kSteps = D / 32;                        // matrix instructions per sub-tile of keys
     constexpr int kVE = D / 16;                           // channels of a value row that a lane loads
@@ -164,16 +176,54 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
     __shared__ __align__(16) float lds[kJoin > kMerge ? kJoin : kMerge];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int kg = lane >> 4, c = lane & 15;
-    const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+    const int g = blockIdx.y;
+    int b, S, n0, n1;                                     // this workgroup's sequence, its splits, the tokens [n0, n1)
+    size_t first, part;                                   // partial of its split 0, and its own
+    if constexpr (!DEALT) {                                 // every sequence in as many splits
+        const int split = blockIdx.x;
+        b = blockIdx.z;
+        S = gridDim.x;
+        const int len = clamped_len(seq_lens, b, N);
+        int chunk = (int)(((long long)len + S - 1) / S);
+        chunk = (chunk + kTokens - 1) / kTokens * kTokens;
+        const long long from = (long long)split * chunk;
+        n0 = (int)(from < len ? from : len);
+        n1 = (int)(from + chunk < len ? from + chunk : len);
+        first = ((size_t)b * p.Hkv + g) * S;
+        part = first + split;
+    } else {
+        // Splits of about as many tokens each, whatever the sequences' lengths: lane i has sequence i, in tiles of 32
+        // tokens.  Every sequence's last split is shorter, so chunks are sized for a few splits less than there are
+        // workgroups: a quarter of B less, or, where that makes too many, twice, three or four times that, which is enough
+        // (of chunks of all / (grid - B) tiles, rounded up, there are grid - B and one more per sequence at most).
+        const unsigned len = lane < p.B ? (unsigned)clamped_lane(seq_lens[lane], N) : 0u, own = (len + kTokens - 1) / kTokens;
+        const unsigned all = __builtin_amdgcn_readlane(wave_upto(own, lane), 63);
+        unsigned pieces = 0, upto = 0;
+        for (unsigned quarter = 1; quarter <= 4; ++quarter) {
+            const unsigned room = gridDim.x - (quarter * (unsigned)p.B + 3) / 4;
+            unsigned chunk = (all + room - 1) / room;
+            chunk = chunk < (unsigned)least ? (unsigned)least : chunk;
+            pieces = lane < p.B ? (own > chunk ? (own + chunk - 1) / chunk : 1u) : 0u;
+            upto = wave_upto(pieces, lane);
+            if (__builtin_amdgcn_readlane(upto, 63) <= gridDim.x) break;
+        }
+        const unsigned long long mine = __ballot(blockIdx.x < upto);
+        if (mine == 0) return;                            // fewer splits than workgroups
+        b = __builtin_ctzll(mine);
+        S = (int)__builtin_amdgcn_readlane(pieces, b);
+        const unsigned before = __builtin_amdgcn_readlane(upto, b) - (unsigned)S, split = blockIdx.x - before;
+        const unsigned total = __builtin_amdgcn_readlane(own, b), step = (total + S - 1) / S;
+        const unsigned end = (split + 1) * step < total ? (split + 1) * step : total;
+        const int n = (int)__builtin_amdgcn_readlane(len, b);
+        n0 = (int)(split * step < total ? split * step : total) * kTokens;
+        n1 = (int)end * kTokens < n ? (int)end * kTokens : n;
+        if (n0 > n1) n0 = n1;
+        first = (size_t)g * gridDim.x + before;
+        part = first + split;
+    }
     const size_t bg = (size_t)b * p.Hkv + g, row0 = (size_t)b * p.Hq + (size_t)g * G;
     arrival_t seen = 0;
     if (S > 1 && t == 0) seen = arrival_peek(p.words + bg * kWordStep);
-
-    const int len = clamped_len(seq_lens, b, N);
-    int chunk = (int)(((long long)len + S - 1) / S);
-    chunk = (chunk + kTokens - 1) / kTokens * kTokens;
-    const long long first = (long long)split * chunk;
-    const int n0 = (int)(first < len ? first : len), n1 = (int)(first + chunk < len ? first + chunk : len);
 
     vec8 qf[kSteps];
     {
@@ -346,7 +396,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
                 if (p.lse2) p.lse2[row0 + h] = total;
             }
         } else {
-            const size_t at_s = (bg * S + split) * G + h;
+            const size_t at_s = part * G + h;
             shared_store(p.part_o + at_s * D + ch, o);
             if (ch == 0) {
                 shared_store(p.part_m + at_s, M - Vec<E>::kLift);
@@ -356,7 +406,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
     }
     if (S == 1) return;
     if (t == 0) arrival_open(p.words + bg * kWordStep, seen, p.nonce);
-    merge_last<E, D, KG, NW>(p, lds, bg, row0);
+    merge_last<E, D, KG, NW>(p, lds, p.words + bg * kWordStep, first, S, row0);
 }
 
 // The step's attention weights, summed over the heads of a KV head, onto the sums of its tokens.
@@ -389,12 +439,20 @@ template <typename E, int D>
 void start(const PagedParams &p, hipStream_t stream)
 {
     constexpr int NW = 8;
-    const dim3 grid((unsigned)p.S, (unsigned)p.Hkv, (unsigned)p.B), block(NW * 64);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p.seq_lens, p.block_table, p.q, p.pages.k, p.pages.v, p.N, (int)p.max_pages, p.G, p.S, p); };
+    const dim3 grid((unsigned)p.S, (unsigned)p.Hkv, p.least ? 1u : (unsigned)p.B), block(NW * 64);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p.seq_lens, p.block_table, p.q, p.pages.k, p.pages.v, p.N, (int)p.max_pages, p.G, p.least, p); };
+    // (LDS and the merge are made for up to 4, 8 or 16 query heads per KV head)
+    auto heads = [&](auto scores, auto dealt) {
+        constexpr bool s = decltype(scores)::value, d = decltype(dealt)::value;
+        p.G <= 4 ? go(paged_attention_kernel<E, D, 4, NW, s, d>)
+                 : (p.G <= 8 ? go(paged_attention_kernel<E, D, 8, NW, s, d>) : go(paged_attention_kernel<E, D, 16, NW, s, d>));
+    };
+    const std::true_type yes{};
+    const std::false_type no{};
     if (p.scores)
-        p.G <= 4 ? go(paged_attention_kernel<E, D, 4, NW, true>) : go(paged_attention_kernel<E, D, 16, NW, true>);
+        p.least ? heads(yes, yes) : heads(yes, no);
     else
-        p.G <= 4 ? go(paged_attention_kernel<E, D, 4, NW, false>) : go(paged_attention_kernel<E, D, 16, NW, false>);
+        p.least ? heads(no, yes) : heads(no, no);
 }
 
 } // namespace

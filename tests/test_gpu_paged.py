@@ -387,3 +387,16 @@ def test_what_is_refused():
     for k, v in ((c.k, c.v[:1]), (c.k, c.v.bfloat16()), (c.k.float(), c.v.float()), (c.k[0], c.v[0]), (c.k[:1].expand_as(c.k), c.v)):
         with pytest.raises(ValueError):
             vb.Pages(k, v)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,N", [(2, 4, 4, 64, 4000), (5, 8, 2, 64, 5003), (9, 4, 1, 64, 4500), (20, 7, 1, 128, 4100), (64, 2, 2, 64, 4001),
+                                          (65, 2, 1, 64, 4001)])
+@pytest.mark.parametrize("how", ["spread", "one", "short", "none"])
+def test_batches_dealt_by_length(B, Hq, Hkv, D, N, how):
+    """Long batches with lengths of their own: sequences in proportion, one that has nearly all tokens, all but empty ones."""
+    c = Cache(B, Hkv, D, 64, N, "bf16", seed=B)
+    g = torch.Generator().manual_seed(B)
+    lens = {"spread": torch.randint(0, N + 1, (B,), generator=g), "one": torch.where(torch.arange(B) == B // 2, N, 3), "short": torch.arange(B) % 3,
+            "none": torch.zeros(B)}[how].int().tolist()
+    w = torch.rand(B, Hkv, N, generator=g).cuda() if B < 20 else None
+    attend(c, c.queries(Hq), lens, weights=w)
