@@ -103,6 +103,29 @@ __device__ __forceinline__ int clamped_len(const int32_t *lens, int b, int N)
 // log2 of the sum, and the sum itself, go to natural units in one place
 __device__ __forceinline__ float natural(float log2_units) { return log2_units * kLn2; }
 
+// 16 bytes of a row.  STREAM: what goes through once need not displace anything from the caches; taken by calls that move
+// more than the 32 MB that the L2 caches hold together.  What a smaller one has written stays in reach of the next call.
+constexpr long long kStreamBytes = 32ll << 20;
+
+typedef unsigned words4 __attribute__((ext_vector_type(4)));
+
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16(const char *row, int piece)
+{
+    const words4 *const p = reinterpret_cast<const words4 *>(row) + piece;
+    return __builtin_bit_cast(uint4, STREAM ? __builtin_nontemporal_load(p) : *p);
+}
+
+template <bool STREAM>
+__device__ __forceinline__ void store16(char *row, int piece, uint4 v)
+{
+    words4 *const p = reinterpret_cast<words4 *>(row) + piece;
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(__builtin_bit_cast(words4, v), p);
+    else
+        *p = __builtin_bit_cast(words4, v);
+}
+
 int launch_rotary_table(const double *freqs, double base, int scaling, double factor, double low, double high,
                         double orig_len, int R, uint64_t *table, hipStream_t stream);
 int launch_rotary(const RotaryParams &p, int bf16, int D, bool append, hipStream_t stream);

@@ -6,8 +6,9 @@
 // upper 32 bits go through sincospi.  The pairs of a token are the same in all heads: a workgroup works the cosines and
 // sines of its tokens out once, into LDS, a thread each.
 //
-// A thread owns 16 channels of a row, 8 pairs: two 16-byte pieces (half layout: R / 2 channels apart; adjacent pairs:
-// side by side).
+// A thread owns 16 channels of a row, 8 pairs: two 16-byte pieces, in the half layout those that belong together, R / 2
+// channels apart, else half of the row (or of what is only copied) apart, so that neighbouring threads' pieces are
+// neighbours.
 #include "paged.h"
 
 namespace vecinfer {
@@ -15,6 +16,7 @@ namespace vecinfer {
 namespace {
 
 constexpr int kBlock = 256;
+constexpr int kMostTokens = 4;                            // of a workgroup
 
 __global__ void rotary_table_kernel(const double *freqs, double base, int scaling, double factor, double low, double high,
                                     double orig_len, int R, uint64_t *table)
@@ -42,41 +44,44 @@ __global__ void rotary_table_kernel(const double *freqs, double base, int scalin
     table[i] = scaled >= 0 && scaled < 18446744073709551616.0 ? (uint64_t)scaled : 0;
 }
 
+// The pairs within a piece (cs: four of them), and those across two (cs: eight).
 template <typename E>
-__device__ __forceinline__ void turn8(uint4 &pa, uint4 &pb, const float2 (&cs)[8], bool interleaved)
+__device__ __forceinline__ void turn_within(uint4 &piece, const float2 *cs)
 {
     typedef E vec8 __attribute__((ext_vector_type(8)));
-    const vec8 a = __builtin_bit_cast(vec8, pa), b = __builtin_bit_cast(vec8, pb);
-    vec8 u, v;
-    if (interleaved) {
+    vec8 v = __builtin_bit_cast(vec8, piece);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float x = (float)a[2 * e], y = (float)a[2 * e + 1];
-            u[2 * e] = (E)fmaf(x, cs[e].x, -(y * cs[e].y));
-            u[2 * e + 1] = (E)fmaf(x, cs[e].y, y * cs[e].x);
-            x = (float)b[2 * e], y = (float)b[2 * e + 1];
-            v[2 * e] = (E)fmaf(x, cs[4 + e].x, -(y * cs[4 + e].y));
-            v[2 * e + 1] = (E)fmaf(x, cs[4 + e].y, y * cs[4 + e].x);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = (float)a[e], y = (float)b[e];
-            u[e] = (E)fmaf(x, cs[e].x, -(y * cs[e].y));
-            v[e] = (E)fmaf(x, cs[e].y, y * cs[e].x);
-        }
+    for (int e = 0; e < 4; ++e) {
+        const float x = (float)v[2 * e], y = (float)v[2 * e + 1];
+        v[2 * e] = (E)fmaf(x, cs[e].x, -(y * cs[e].y));
+        v[2 * e + 1] = (E)fmaf(x, cs[e].y, y * cs[e].x);
     }
-    pa = __builtin_bit_cast(uint4, u);
-    pb = __builtin_bit_cast(uint4, v);
+    piece = __builtin_bit_cast(uint4, v);
+}
+
+template <typename E>
+__device__ __forceinline__ void turn_across(uint4 &one, uint4 &two, const float2 *cs)
+{
+    typedef E vec8 __attribute__((ext_vector_type(8)));
+    const vec8 a = __builtin_bit_cast(vec8, one), b = __builtin_bit_cast(vec8, two);
+    vec8 u, v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = (float)a[e], y = (float)b[e];
+        u[e] = (E)fmaf(x, cs[e].x, -(y * cs[e].y));
+        v[e] = (E)fmaf(x, cs[e].y, y * cs[e].x);
+    }
+    one = __builtin_bit_cast(uint4, u);
+    two = __builtin_bit_cast(uint4, v);
 }
 
 // grid (tokens / TPW, head groups); TPW tokens per workgroup, 1 << tpw_shift
-template <typename E, int D, bool APPEND>
+template <typename E, int D, bool APPEND, bool STREAM>
 __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, int tpw_shift)
 {
     constexpr int kUnits = D / 16;                        // threads per row
     constexpr int kRows = kBlock / kUnits;                // rows at a time
-    __shared__ float2 cs_s[4 * (D / 2)];
+    __shared__ float2 cs_s[kMostTokens * (D / 2)];
     const int t = threadIdx.x, u = t % kUnits, row = t / kUnits;
     const int tpw = 1 << tpw_shift, half = p.R / 2;
     const unsigned tok0 = blockIdx.x << tpw_shift, n_tok = (unsigned)p.B * (unsigned)p.T;
@@ -108,19 +113,29 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, in
     const unsigned tok = tok0 + k;
     if (tok >= n_tok) return;
     const unsigned b = tok / (unsigned)p.T, at = tok - b * (unsigned)p.T;
-    const bool turned = u < p.R / 16;
-    int c0, c1;                                           // the two 16-byte pieces
-    if (turned && !p.interleaved) {
-        c0 = u;
-        c1 = u + p.R / 16;
-    } else {
-        c0 = 2 * u;                                       // (behind the turned channels as well)
-        c1 = c0 + 1;
-    }
+    int c0, c1;                                           // the two pieces
+    bool turn0, turn1;
     float2 cs[8];
-    if (turned)
+    if (p.interleaved) {
+        c0 = u;
+        c1 = u + kUnits;
+        turn0 = 8 * c0 < p.R;
+        turn1 = 8 * c1 < p.R;
+        if (turn0)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) cs[e] = cs_s[k * half + 8 * u + e];
+            for (int e = 0; e < 4; ++e) cs[e] = cs_s[k * half + 4 * c0 + e];
+        if (turn1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cs[4 + e] = cs_s[k * half + 4 * c1 + e];
+    } else {
+        const int pairs = p.R / 16;                       // of pieces
+        turn0 = turn1 = u < pairs;
+        c0 = u < pairs ? u : u + pairs;
+        c1 = u < pairs ? u + pairs : u + kUnits;
+        if (turn0)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cs[e] = cs_s[k * half + 8 * u + e];
+    }
 
     char *k_out = nullptr, *v_out = nullptr;
     long long where = -1;
@@ -144,7 +159,7 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, in
     for (int h = (row >> tpw_shift) + step * blockIdx.y; h < heads; h += step * gridDim.y) {
         const char *in;
         char *out;
-        bool turn = turned;
+        bool turn = true;
         if (!APPEND || h < p.x.heads) {
             in = p.x.in + b * p.x.in_b + h * p.x.in_h + at * p.x.in_t;
             out = p.x.out + b * p.x.out_b + h * p.x.out_h + at * p.x.out_t;
@@ -161,24 +176,49 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, in
             out = v_out + (unsigned long long)g * p.pages.v_head;
             turn = false;
         }
-        uint4 a = reinterpret_cast<const uint4 *>(in)[c0], bb = reinterpret_cast<const uint4 *>(in)[c1];
-        if (turn) turn8<E>(a, bb, cs, p.interleaved);
-        reinterpret_cast<uint4 *>(out)[c0] = a;
-        reinterpret_cast<uint4 *>(out)[c1] = bb;
+        uint4 one = load16<STREAM>(in, c0), two = load16<STREAM>(in, c1);
+        if (turn) {
+            if (p.interleaved) {
+                if (turn0) turn_within<E>(one, cs);
+                if (turn1) turn_within<E>(two, cs + 4);
+            } else if (turn0) {
+                turn_across<E>(one, two, cs);
+            }
+        }
+        store16<STREAM>(out, c0, one);
+        store16<STREAM>(out, c1, two);
     }
 }
 
+// Tokens per workgroup: 1, 2 or 4, as few as leave the fewest threads idle - its rows are then dealt to the heads of a token
+// (8192 tokens, 32 heads: 24.4 us with one token, 25.5 with four; 48 heads of an append: 30.0 with two, 30.8 with four, 38
+// with one; 8 heads 11.2 with four, 14.0 with one).  Where there are fewer tokens than would fill the chip, one, and a
+// token's heads are dealt to several workgroups.
+// Streaming (load16): 8192 tokens 25.5 us, 29.0 otherwise; 2048 9.0 and 10.0; 512 no difference.
 template <typename E, int D, bool APPEND>
 void start(const RotaryParams &p, hipStream_t stream)
 {
+    constexpr int kRows = kBlock / (D / 16);
     const long long n_tok = (long long)p.B * p.T;
-    const int tpw_shift = n_tok >= 4 * (long long)num_cus() ? 2 : 0;
     const int heads = p.x.heads + (APPEND ? p.k.heads + p.v.heads : 0);
-    const int step = (kBlock / (D / 16)) >> tpw_shift;
-    const int passes = (heads + step - 1) / step;
-    const unsigned gx = (unsigned)((n_tok + (1 << tpw_shift) - 1) >> tpw_shift);
-    const unsigned gy = tpw_shift ? 1 : (unsigned)(passes < 65535 ? passes : 65535);
-    hipLaunchKernelGGL((rotary_kernel<E, D, APPEND>), dim3(gx, gy), dim3(kBlock), 0, stream, p, tpw_shift);
+    auto rows_taken = [&](int shift) {                    // by one token's heads, idle ones included
+        const int step = kRows >> shift;
+        return (heads + step - 1) / step * step;
+    };
+    int shift = 0;
+    unsigned gy = 1;
+    if (n_tok >= 4 * (long long)num_cus()) {
+        for (int i = 1; 1 << i <= kMostTokens; ++i)
+            if (rows_taken(i) < rows_taken(shift)) shift = i;
+    } else {
+        const int passes = rows_taken(0) / kRows;
+        gy = (unsigned)(passes < 65535 ? passes : 65535);
+    }
+    const dim3 grid((unsigned)((n_tok + (1 << shift) - 1) >> shift), gy);
+    if (4 * n_tok * heads * D >= kStreamBytes)
+        hipLaunchKernelGGL((rotary_kernel<E, D, APPEND, true>), grid, dim3(kBlock), 0, stream, p, shift);
+    else
+        hipLaunchKernelGGL((rotary_kernel<E, D, APPEND, false>), grid, dim3(kBlock), 0, stream, p, shift);
 }
 
 } // namespace

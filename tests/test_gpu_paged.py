@@ -355,6 +355,12 @@ def test_append_many(B, T):
     append(c, T, [T] * B, rot=vb.Rotary(64, 32), Hq=4)
 
 
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+def test_append_more_than_the_caches_hold(dtype):
+    c = Cache(2, 8, 128, 32, 1100, dtype, fill=False)
+    append(c, 1050, [1100, 900], [1050, 650], rot=vb.Rotary(128, 128), Hq=24)
+
+
 def test_append_clears_weights():
     c = Cache(2, 2, 64, 16, 96)
     w = torch.rand(2, 2, 90, generator=c.g).cuda() + 1
