@@ -161,11 +161,12 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, arr
     }
 }
 
-// (what the first requests need comes first: the command processor puts the leading arguments into registers)
+// What the way to the first page needs comes first: the command processor puts the leading 14 dwords into registers, and
+// what lies behind them arrives while the length and the page travel (packed: G, the pages' shift and, dealt by length, B).
 template <typename E, int D, int KG, int NW, bool SCORES, bool DEALT>
 __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t *seq_lens, const int32_t *block_table, const char *q,
-                                                                  const char *k_pool, const char *v_pool, int N, int max_pages, int G,
-                                                                  int least, const PagedParams p)
+                                                                  const char *k_pool, const char *v_pool, int N, int max_pages,
+                                                                  unsigned packed, int parts, const PagedParams p)
 {
     constexpr int kSteps = D / 32;                        // matrix instructions per sub-tile of keys
     constexpr int kVE = D / 16;                           // channels of a value row that a lane loads
@@ -176,13 +177,14 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
     __shared__ __align__(16) float lds[kJoin > kMerge ? kJoin : kMerge];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int kg = lane >> 4, c = lane & 15;
+    const int G = packed & 0xff, shift = packed >> 8 & 0xff, B = packed >> 16;
     const int g = blockIdx.y;
     int b, S, n0, n1;                                     // this workgroup's sequence, its splits, the tokens [n0, n1)
     size_t first, part;                                   // partial of its split 0, and its own
     if constexpr (!DEALT) {                                 // every sequence in as many splits
         const int split = blockIdx.x;
         b = blockIdx.z;
-        S = gridDim.x;
+        S = parts;
         const int len = clamped_len(seq_lens, b, N);
         int chunk = (int)(((long long)len + S - 1) / S);
         chunk = (chunk + kTokens - 1) / kTokens * kTokens;
@@ -196,16 +198,16 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
         // tokens.  Every sequence's last split is shorter, so chunks are sized for a few splits less than there are
         // workgroups: a quarter of B less, or, where that makes too many, twice, three or four times that, which is enough
         // (of chunks of all / (grid - B) tiles, rounded up, there are grid - B and one more per sequence at most).
-        const unsigned len = lane < p.B ? (unsigned)clamped_lane(seq_lens[lane], N) : 0u, own = (len + kTokens - 1) / kTokens;
+        const unsigned len = lane < B ? (unsigned)clamped_lane(seq_lens[lane], N) : 0u, own = (len + kTokens - 1) / kTokens;
         const unsigned all = __builtin_amdgcn_readlane(wave_upto(own, lane), 63);
         unsigned pieces = 0, upto = 0;
         for (unsigned quarter = 1; quarter <= 4; ++quarter) {
-            const unsigned room = gridDim.x - (quarter * (unsigned)p.B + 3) / 4;
+            const unsigned room = (unsigned)parts - (quarter * (unsigned)B + 3) / 4;
             unsigned chunk = (all + room - 1) / room;
-            chunk = chunk < (unsigned)least ? (unsigned)least : chunk;
-            pieces = lane < p.B ? (own > chunk ? (own + chunk - 1) / chunk : 1u) : 0u;
+            chunk = chunk < (unsigned)p.least ? (unsigned)p.least : chunk;
+            pieces = lane < B ? (own > chunk ? (own + chunk - 1) / chunk : 1u) : 0u;
             upto = wave_upto(pieces, lane);
-            if (__builtin_amdgcn_readlane(upto, 63) <= gridDim.x) break;
+            if (__builtin_amdgcn_readlane(upto, 63) <= (unsigned)parts) break;
         }
         const unsigned long long mine = __ballot(blockIdx.x < upto);
         if (mine == 0) return;                            // fewer splits than workgroups
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
         n0 = (int)(split * step < total ? split * step : total) * kTokens;
         n1 = (int)end * kTokens < n ? (int)end * kTokens : n;
         if (n0 > n1) n0 = n1;
-        first = (size_t)g * gridDim.x + before;
+        first = (size_t)g * (unsigned)parts + before;
         part = first + split;
     }
     const size_t bg = (size_t)b * p.Hkv + g, row0 = (size_t)b * p.Hq + (size_t)g * G;
@@ -237,7 +239,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
     }
 
     const int32_t *const pages = block_table + (size_t)b * max_pages;
-    const int shift = p.pages.shift, last_col = (N - 1) >> shift;
+    const int last_col = (N - 1) >> shift;
     const unsigned slot_mask = (1u << shift) - 1;
     const char *const k0 = k_pool + (size_t)g * p.pages.k_head, *const v0 = v_pool + (size_t)g * p.pages.v_head;
     const int krow = 8 * (c >> 2) + (c & 3);              // this lane's key token of sub-tile 0; of sub-tile 1: + 4
@@ -440,7 +442,10 @@ void start(const PagedParams &p, hipStream_t stream)
 {
     constexpr int NW = 8;
     const dim3 grid((unsigned)p.S, (unsigned)p.Hkv, p.least ? 1u : (unsigned)p.B), block(NW * 64);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p.seq_lens, p.block_table, p.q, p.pages.k, p.pages.v, p.N, (int)p.max_pages, p.G, p.least, p); };
+    const unsigned packed = (unsigned)p.G | (unsigned)p.pages.shift << 8 | (p.least ? (unsigned)p.B << 16 : 0u);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, stream, p.seq_lens, p.block_table, p.q, p.pages.k, p.pages.v, p.N, (int)p.max_pages, packed, p.S, p);
+    };
     // (LDS and the merge are made for up to 4, 8 or 16 query heads per KV head)
     auto heads = [&](auto scores, auto dealt) {
         constexpr bool s = decltype(scores)::value, d = decltype(dealt)::value;
