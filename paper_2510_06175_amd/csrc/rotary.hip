@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, in
 // (8192 tokens, 32 heads: 24.4 us with one token, 25.5 with four; 48 heads of an append: 30.0 with two, 30.8 with four, 38
 // with one; 8 heads 11.2 with four, 14.0 with one).  Where there are fewer tokens than would fill the chip, one, and a
 // token's heads are dealt to several workgroups.
-// Streaming (load16): 8192 tokens 25.5 us, 29.0 otherwise; 2048 9.0 and 10.0; 512 no difference.
+// Streaming (load16): 8192 tokens out of memory 25.5 us, 29.0 otherwise; 512 no difference.
 template <typename E, int D, bool APPEND>
 void start(const RotaryParams &p, hipStream_t stream)
 {

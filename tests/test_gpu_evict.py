@@ -120,6 +120,12 @@ def test_many_long_rows():
     evict(c, weights(c, 20000, "ties"), 300, 3, 40, lens=[20000 - 700 * i for i in range(24)])
 
 
+@pytest.mark.parametrize("D,B,keep", [(128, 4, 2103), (64, 8, 2103)])
+def test_more_than_the_caches_hold(D, B, keep):
+    c = Cache(B, 8, D, 32, 4003, token_major=D == 64, seed=D)
+    evict(c, weights(c, 4003), keep, 4, 100, lens=[4003 - 300 * i for i in range(B)], dP=64)
+
+
 def test_special_weights():
     """-0 equals 0, infinities are ordered, what is no number comes below them, and ties go to the lowest index."""
     c = Cache(1, 1, 64, 8, 12)

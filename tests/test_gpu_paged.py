@@ -357,8 +357,8 @@ def test_append_many(B, T):
 
 @pytest.mark.parametrize("dtype", ref.DTYPES)
 def test_append_more_than_the_caches_hold(dtype):
-    c = Cache(2, 8, 128, 32, 1100, dtype, fill=False)
-    append(c, 1050, [1100, 900], [1050, 650], rot=vb.Rotary(128, 128), Hq=24)
+    c = Cache(2, 8, 128, 32, 1800, dtype, fill=False)
+    append(c, 1750, [1800, 1400], [1750, 650], rot=vb.Rotary(128, 128), Hq=24)
 
 
 def test_append_clears_weights():

@@ -51,7 +51,7 @@ def test_sizes(B, H, T, D):
     check(rot, rows(g, B, H, T, D, torch.bfloat16), torch.arange(T).expand(B, T) + 11, explicit=False, pos0=11)
 
 
-@pytest.mark.parametrize("B,H,T,D,R,interleaved", [(1, 40, 2203, 128, 128, 0), (2, 33, 1103, 128, 80, 1), (3, 5, 8191, 128, 48, 0), (1, 64, 2500, 64, 64, 1)])
+@pytest.mark.parametrize("B,H,T,D,R,interleaved", [(1, 40, 3503, 128, 128, 0), (2, 33, 2103, 128, 80, 1), (3, 5, 9191, 128, 48, 0), (1, 64, 4500, 64, 64, 1)])
 def test_more_than_the_caches_hold(B, H, T, D, R, interleaved):
     g = torch.Generator().manual_seed(T)
     check(vb.Rotary(D, R, interleaved, base=500000.0), rows(g, B, H, T, D, torch.float16), torch.randint(0, 9000, (B, T), generator=g), inverse=1)
