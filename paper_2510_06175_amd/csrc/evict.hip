@@ -41,7 +41,7 @@ struct __attribute__((packed, aligned(4))) Four {
 
 struct Shared {
     unsigned hist[kBins * kCopies];
-    unsigned above[kWaves], equal[kWaves], sums[kWaves];
+    __align__(16) unsigned above[kWaves], equal[kWaves], sums[kWaves];
     unsigned pick[2];
     unsigned all[kWaves][kGroups], mine[kWaves][kGroups];
 };
@@ -155,14 +155,16 @@ __device__ __forceinline__ void own_bins(const Shared &s, unsigned (&h)[2])
     }
 }
 
-__device__ __forceinline__ unsigned wave_prefix(unsigned v, int lane)       // inclusive
+// Sum of the wavefronts' counts before this one's.
+__device__ __forceinline__ unsigned before_wave(const unsigned (&counts)[kWaves], int wave)
 {
+    unsigned sum = 0;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned x = __shfl_up(v, o);
-        if (lane >= o) v += x;
+    for (int w = 0; w < kWaves; w += 4) {
+        const uint4 c = *reinterpret_cast<const uint4 *>(counts + w);
+        sum += (w < wave ? c.x : 0u) + (w + 1 < wave ? c.y : 0u) + (w + 2 < wave ? c.z : 0u) + (w + 3 < wave ? c.w : 0u);
     }
-    return v;
+    return sum;
 }
 
 // The bin (h: this thread's two) at which, counted from the top, the room ends: returned, and the tokens above it taken
@@ -170,15 +172,14 @@ __device__ __forceinline__ unsigned wave_prefix(unsigned v, int lane)       // i
 __device__ __forceinline__ unsigned find_bin(Shared &s, const unsigned (&h)[2], unsigned &room)
 {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const unsigned upto = wave_prefix(h[0] + h[1], lane);
+    const unsigned upto = wave_upto(h[0] + h[1]);
     if (lane == 63) s.sums[wave] = upto;
     if (t == 0) {
         s.pick[0] = kBins;
         s.pick[1] = 0;
     }
     __syncthreads();
-    unsigned before = upto - h[0] - h[1];
-    for (int w = 0; w < wave; ++w) before += s.sums[w];
+    unsigned before = upto - h[0] - h[1] + before_wave(s.sums, wave);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if (before <= room && room < before + h[i]) {     // (one bin of all)
@@ -218,7 +219,7 @@ __device__ __forceinline__ unsigned find_bin_of_parts(Shared &s, const unsigned 
         total += s.all[w][lane];
         before += s.mine[w][lane];
     }
-    const unsigned upto = wave_prefix(total, lane), from_top = upto - total, mine_upto = wave_prefix(before, lane);
+    const unsigned upto = wave_upto(total), from_top = upto - total, mine_upto = wave_upto(before);
     const unsigned long long here = __ballot(from_top <= room && room < upto);
     if (here == 0) {                                      // there is room for all
         more = __shfl(mine_upto, 63);
@@ -253,7 +254,7 @@ __device__ __forceinline__ unsigned find_bin_of_parts(Shared &s, const unsigned 
             total += s.all[w][lane];
             before += s.mine[w][lane];
         }
-    const unsigned bin_upto = above + wave_prefix(total, lane), bin_top = bin_upto - total, mine_bin = wave_prefix(before, lane);
+    const unsigned bin_upto = above + wave_upto(total), bin_top = bin_upto - total, mine_bin = wave_upto(before);
     const int at = __builtin_ctzll(__ballot(bin_top <= room && room < bin_upto));
     more += __shfl(mine_bin - before, at);
     same = __shfl(before, at);
@@ -281,10 +282,8 @@ __device__ __forceinline__ void list_kept(Shared &s, Stretch &x, const EvictPara
         s.equal[wave] = equal;
     }
     __syncthreads();
-    for (int w = 0; w < wave; ++w) {
-        taken += s.above[w];
-        ties += s.equal[w];
-    }
+    taken += before_wave(s.above, wave);
+    ties += before_wave(s.equal, wave);
     taken += ties < room ? ties : room;
     const unsigned long long lower = ~(~0ull << lane);
     x.each([&](int i, const unsigned(&k)[4]) {

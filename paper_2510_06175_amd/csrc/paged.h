@@ -3,6 +3,8 @@
 #pragma once
 #include "common.h"
 
+#include <type_traits>
+
 namespace vecinfer {
 
 typedef _Float16 f16;
@@ -98,6 +100,23 @@ __device__ __forceinline__ int clamped_len(const int32_t *lens, int b, int N)
     typedef const int32_t __attribute__((address_space(4))) *const_i32_ptr;
     const int v = ((const_i32_ptr)(uintptr_t)lens)[b];
     return clamped_lane(v, N);
+}
+
+// Sum over the lanes of the wavefront up to this one, on the vector ALU (DPP): within the rows of 16 lanes, then each
+// row's last lane into the rows behind it.
+__device__ __forceinline__ unsigned wave_upto(unsigned v)
+{
+    auto from = [&](auto ctrl, auto rows) {
+        return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    };
+    using std::integral_constant;
+    v += from(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});      // row_shr:1
+    v += from(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});      // row_shr:2
+    v += from(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});      // row_shr:4
+    v += from(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});      // row_shr:8
+    v += from(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});      // row_bcast:15 into rows 1 and 3
+    v += from(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});      // row_bcast:31 into rows 2 and 3
+    return v;
 }
 
 // log2 of the sum, and the sum itself, go to natural units in one place

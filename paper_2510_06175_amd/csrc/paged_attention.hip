@@ -61,17 +61,6 @@ __device__ __forceinline__ typename Vec<E>::v8 as_vec(unsigned a, unsigned b, un
     return __builtin_bit_cast(typename Vec<E>::v8, u);
 }
 
-// Sum over the lanes up to this one.
-__device__ __forceinline__ unsigned wave_upto(unsigned v, int lane)
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned x = __shfl_up(v, o);
-        if (lane >= o) v += x;
-    }
-    return v;
-}
-
 // Called by all threads of a workgroup whose partials are stored: the last of the S workgroups of this (sequence, KV
 // head) writes the output rows (split_merge.h).  The rows of the first kBatch splits travel while the weights are
 // worked out, a wavefront per head.
@@ -206,14 +195,14 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
         // workgroups: a quarter of B less, or, where that makes too many, twice, three or four times that, which is enough
         // (of chunks of all / (grid - B) tiles, rounded up, there are grid - B and one more per sequence at most).
         const unsigned len = lane < B ? (unsigned)clamped_lane(seq_lens[lane], N) : 0u, own = (len + kTokens - 1) / kTokens;
-        const unsigned all = __builtin_amdgcn_readlane(wave_upto(own, lane), 63);
+        const unsigned all = __builtin_amdgcn_readlane(wave_upto(own), 63);
         unsigned pieces = 0, upto = 0;
         for (unsigned quarter = 1; quarter <= 4; ++quarter) {
             const unsigned room = (unsigned)parts - (quarter * (unsigned)B + 3) / 4;
             unsigned chunk = (all + room - 1) / room;
             chunk = chunk < (unsigned)p.least ? (unsigned)p.least : chunk;
             pieces = lane < B ? (own > chunk ? (own + chunk - 1) / chunk : 1u) : 0u;
-            upto = wave_upto(pieces, lane);
+            upto = wave_upto(pieces);
             if (__builtin_amdgcn_readlane(upto, 63) <= (unsigned)parts) break;
         }
         const unsigned long long mine = __ballot(blockIdx.x < upto);
