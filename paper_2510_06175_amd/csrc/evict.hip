@@ -6,12 +6,14 @@
 // digits of 11, 11 and 10 bits: a histogram of the tokens that agree with T so far, and the bin at which, counted from the
 // top, the room ends.  Then the tokens above T, and as many of those equal to it, lowest index first, as there is room for,
 // are listed in order.
-// What bounds it is issue: some 70 vector instructions per token, of which one compute unit does 64 lanes per cycle.  So a
-// row of up to kHeld tokens, whose keys fit a workgroup's registers, is one workgroup's in one launch, and a longer one is
-// cut into up to kMaxParts stretches, a launch per digit and one for the list, through a histogram per stretch: each
-// workgroup of the next launch adds them up for itself, which needs no atomics, no clearing and no order of workgroups.
+// What bounds it is issue: some 70 vector instructions per token, of which one compute unit does 64 lanes per cycle, and
+// for short rows the steps themselves (500 tokens 7 us, 8192 9.8, 32000 22).  So a row of up to kHeld tokens, whose keys fit
+// a workgroup's registers, is one workgroup's in one launch, and a longer one is cut into up to kMaxParts stretches, a launch
+// per digit and one for the list, through a histogram per stretch: each workgroup of the next launch adds them up for
+// itself, which needs no atomics, no clearing and no order of workgroups (100003 tokens: 27 us in four launches; by one
+// workgroup, the row read again for each digit, 89).
 // The move: 16 lanes per row of a kept token, keys and values; bound by memory (32768 of 100003 tokens, 8 KV heads, 268 MB:
-// 43 us, 48 without streaming)
+// 52 us, the rate of a large copy).
 #include "paged.h"
 
 namespace vecinfer {
@@ -21,9 +23,12 @@ namespace {
 constexpr int kSelect = 1024, kWaves = kSelect / 64;
 constexpr int kBins = 2048;
 constexpr int kCopies = 4;                                // of a histogram in LDS: neighbouring lanes count apart
-constexpr int kTurns = 4;                                 // of 256 tokens per wavefront whose keys are held in registers
-constexpr int kHeld = kSelect * 4 * kTurns;               // tokens of a workgroup that are read once
-constexpr int kPart = kHeld / 2;                          // tokens of a stretch, unless that makes too many
+// Turns of 256 tokens per wavefront whose keys are held in registers, by a workgroup that has a row for itself (1, 2, 4 or
+// 8, as the row needs: 4000 tokens 14.2 us with one, 15.1 with eight) and by one that shares it: so many are read once (one
+// sequence of 20000 tokens, 8 KV heads, keeping 2000: 24.2 us by a workgroup per row, 33.3 shared; 32000 30.3 and 33.6).
+constexpr int kTurnsWhole = 8, kTurnsPart = 4;
+constexpr int kHeld = kSelect * 4 * kTurnsWhole, kHeldPart = kSelect * 4 * kTurnsPart;
+constexpr int kPart = kHeldPart / 2;                      // tokens of a stretch, unless that makes too many
 constexpr int kMaxParts = 64;
 constexpr int kGroup = 32, kGroups = kBins / kGroup, kHist = kBins + kGroups;    // a stretch's histogram in memory
 
@@ -47,6 +52,7 @@ struct Shared {
 };
 
 // What a workgroup knows of its tokens [from, to) of a row, of which this wavefront has [mine, mine_to).
+template <int kTurns>
 struct Stretch {
     const float *w;
     const int32_t *pages;
@@ -120,8 +126,8 @@ __device__ __forceinline__ void clear_hist(Shared &s)
 }
 
 // Histogram of the next digit over the tokens whose digits so far are `prefix`.  Ends behind a barrier.
-template <int DIGIT>
-__device__ __forceinline__ void count_digit(Shared &s, Stretch &x, unsigned prefix)
+template <int DIGIT, int kTurns>
+__device__ __forceinline__ void count_digit(Shared &s, Stretch<kTurns> &x, unsigned prefix)
 {
     constexpr int kAt = DIGIT == 1 ? 21 : (DIGIT == 2 ? 10 : 0);
     constexpr unsigned kMask = DIGIT == 3 ? 1023u : 2047u;
@@ -264,7 +270,8 @@ __device__ __forceinline__ unsigned find_bin_of_parts(Shared &s, const unsigned 
 
 // The list of what stays: tokens above T and, of those equal to it, the first `room` of the row.  `taken` stay and `ties`
 // are equal to T in front of this workgroup's tokens (T = 0: all that are there stay, room = 0).
-__device__ __forceinline__ void list_kept(Shared &s, Stretch &x, const EvictParams &p, int g, int b, bool last, unsigned T, unsigned room,
+template <int kTurns>
+__device__ __forceinline__ void list_kept(Shared &s, Stretch<kTurns> &x, const EvictParams &p, int g, int b, bool last, unsigned T, unsigned room,
                                           unsigned taken, unsigned ties)
 {
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -320,11 +327,12 @@ __device__ __forceinline__ void list_kept(Shared &s, Stretch &x, const EvictPara
 }
 
 // A row per workgroup: grid (KV heads, sequences).
+template <int TURNS>
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(const EvictParams p)
 {
     __shared__ __align__(16) Shared s;
     const int g = blockIdx.x, b = blockIdx.y;
-    Stretch x;
+    Stretch<TURNS> x;
     x.open(p, g, b, 0, 1);
     unsigned h[2], room = (unsigned)p.keep, T = 0;
     count_digit<1>(s, x, 0);
@@ -356,7 +364,7 @@ __global__ __launch_bounds__(kSelect) void evict_stage_kernel(const EvictParams 
     const size_t row = (size_t)b * p.Hkv + g, rows = (size_t)p.B * p.Hkv;
     unsigned *const hists = p.hists + row * parts * kHist;
     unsigned *const state = p.states + (row * parts + part) * 3;
-    Stretch x;
+    Stretch<kTurnsPart> x;
     x.open(p, g, b, part, parts);
     unsigned found = 0, room = (unsigned)p.keep, taken = 0, ties = 0;
     bool all = false;
@@ -428,7 +436,7 @@ int evict_parts(long long rows, long long N)
 {
     if (N <= kHeld) return 1;
     long long parts = (N + kPart - 1) / kPart;
-    if (rows * parts > 4 * num_cus()) parts = (N + kHeld - 1) / kHeld;     // the rows alone fill the chip
+    if (rows * parts > 4 * num_cus()) parts = (N + kHeldPart - 1) / kHeldPart;     // the rows alone fill the chip
     return (int)(parts < kMaxParts ? parts : kMaxParts);
 }
 
@@ -448,7 +456,12 @@ int launch_evict(const EvictParams &p, hipStream_t stream)
 {
     const int parts = evict_parts((long long)p.B * p.Hkv, p.N);
     if (parts == 1) {
-        hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)p.Hkv, (unsigned)p.B), dim3(kSelect), 0, stream, p);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)p.Hkv, (unsigned)p.B), dim3(kSelect), 0, stream, p); };
+        const int turns = (p.N + 4 * kSelect - 1) / (4 * kSelect);
+        turns <= 1 ? go(evict_select_kernel<1>)
+        : turns <= 2 ? go(evict_select_kernel<2>)
+        : turns <= 4 ? go(evict_select_kernel<4>)
+                     : go(evict_select_kernel<kTurnsWhole>);
     } else {
         const dim3 grid((unsigned)parts, (unsigned)p.Hkv, (unsigned)p.B);
         hipLaunchKernelGGL(evict_stage_kernel<1>, grid, dim3(kSelect), 0, stream, p);

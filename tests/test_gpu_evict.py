@@ -102,7 +102,8 @@ def test_long(N, how):
     evict(c, weights(c, N, how), N // 3, 10, N // 6)
 
 
-@pytest.mark.parametrize("N,lens", [(16384, [16384, 16383, 1]), (16385, [16385, 0, 300]), (40000, [40000, 39999, 8191, 8193, 16384, 5])])
+@pytest.mark.parametrize("N,lens", [(16385, [16385, 16384, 1]), (32768, [32768, 16383, 1]), (32769, [32769, 0, 300]),
+                                    (40000, [40000, 39999, 8191, 8193, 16384, 5])])
 @pytest.mark.parametrize("how", ["zero", "bits", "close"])
 def test_rows_of_one_or_more_workgroups(N, lens, how):
     c = Cache(len(lens), 1, 64, 1024, N, seed=N)
