@@ -436,7 +436,7 @@ typedef struct vecinfer_rotary_cfg {
     double factor;         /* > 0; scaling other than PLAIN                                             */
     double low_turns, high_turns;   /* PARTS: low < high                                                */
     int64_t orig_len;      /* PARTS: tokens of the original context, >= 1                               */
-    double magnitude;      /* m: factor of cosine and sine (1: lengths are kept), finite                */
+    double magnitude;      /* m: factor of cosine and sine (1: lengths are kept), finite in fp32        */
 } vecinfer_rotary_cfg;
 
 /*
@@ -457,7 +457,8 @@ int vecinfer_rotary_table(const vecinfer_rotary_cfg *cfg, const double *freqs, u
  *   x, out     [B, H, T, D] by strides {b, h, t}; out may be x itself (same strides), else they may not overlap
  *   positions  int32 [B, T] on the device, or NULL: token t has position pos0 + t
  * Errors: EINVAL for null or misaligned pointers, B, H or T < 1, dtype or strides outside the ranges above,
- * and a cfg as for vecinfer_rotary_table; EUNSUPPORTED for its head_dim or rot_dim, and B T >= 2^31.
+ * and a cfg as for vecinfer_rotary_table; EUNSUPPORTED for its head_dim or rot_dim, H above 65535,
+ * and B T >= 2^31.
  */
 int vecinfer_rotary(const vecinfer_rotary_cfg *cfg, const uint64_t *table, int32_t dtype, const void *x,
                     const int64_t x_strides[3], void *out, const int64_t out_strides[3], int32_t B, int32_t H,
@@ -495,7 +496,8 @@ typedef struct vecinfer_pages {
  *   weights       fp32 [B, H_kv, w_cap] or NULL: the sums of vecinfer_paged_attention, set to 0 for the new
  *                 tokens below w_cap
  * Errors: EINVAL (null or misaligned pointers, sizes < 1, strides, q without rot or without q_out, pages or
- * cfg outside their ranges, different head_dim), EUNSUPPORTED (head_dim, rot_dim, page_size; B T >= 2^31).
+ * cfg outside their ranges, different head_dim), EUNSUPPORTED (head_dim, rot_dim, page_size, H_q or H_kv
+ * above 65535, B T >= 2^31).
  */
 int vecinfer_paged_append(const vecinfer_pages *pages, const vecinfer_rotary_cfg *rot, const uint64_t *table,
                           const void *k_new, const int64_t k_strides[3], const void *v_new,
@@ -529,7 +531,7 @@ size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q
  *              (holes: + 0).  weights_in may be weights_out, or NULL: 0.  Rows t >= len_b are left as they
  *              were.  With weights a second launch follows.
  *   workspace  as for vecinfer_decode_attention
- * Errors: EINVAL (null or misaligned pointers, sizes, strides, scale not finite, w_cap < N, weights_in alone),
+ * Errors: EINVAL (null or misaligned pointers, sizes, strides, scale (or scale log2 e) not finite, w_cap < N, weights_in alone),
  * EUNSUPPORTED (pages, G, B or H_kv above 65535, N > 2^30, max_pages >= 2^31), EWORKSPACE, ELAUNCH.
  */
 int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const int64_t q_strides[2],

@@ -24,7 +24,7 @@ int rotary_ok(const vecinfer_rotary_cfg *c)
     if (c->rot_dim < 16 || c->rot_dim > c->head_dim || c->rot_dim % 16) return VECINFER_EUNSUPPORTED;
     if ((c->interleaved != 0 && c->interleaved != 1) || c->scaling < VECINFER_ROTARY_PLAIN || c->scaling > VECINFER_ROTARY_PARTS)
         return VECINFER_EINVAL;
-    if (!(c->base > 0) || !isfinite(c->base) || !isfinite(c->magnitude)) return VECINFER_EINVAL;
+    if (!(c->base > 0) || !isfinite(c->base) || !isfinite((float)c->magnitude)) return VECINFER_EINVAL;
     if (c->scaling != VECINFER_ROTARY_PLAIN && (!(c->factor > 0) || !isfinite(c->factor))) return VECINFER_EINVAL;
     if (c->scaling == VECINFER_ROTARY_PARTS &&
         (!(c->low_turns < c->high_turns) || !isfinite(c->low_turns) || !isfinite(c->high_turns) || c->orig_len < 1))
@@ -32,8 +32,7 @@ int rotary_ok(const vecinfer_rotary_cfg *c)
     return VECINFER_OK;
 }
 
-// Steps of a tensor: not negative, whole 16-byte pieces, and so small that no offset of int64 elements wraps
-// for sizes below 2^31 per axis.
+// Steps of a tensor: not negative, whole 16-byte pieces.
 bool strides_ok(const int64_t *s, int n, int64_t below)
 {
     for (int i = 0; i < n; ++i)
@@ -201,7 +200,7 @@ int vecinfer_rotary(const vecinfer_rotary_cfg *cfg, const uint64_t *table, int32
     if (B < 1 || H < 1 || T < 1) return VECINFER_EINVAL;
     if (!aligned(x, 16) || !aligned(out, 16) || !aligned(table, 8) || !aligned(positions, 4)) return VECINFER_EINVAL;
     if (!strides_ok(x_strides, 3, kStride) || !strides_ok(out_strides, 3, kStride)) return VECINFER_EINVAL;
-    if (T > 0x7fffffffLL / B) return VECINFER_EUNSUPPORTED;
+    if (T > 0x7fffffffLL / B || H > 65535) return VECINFER_EUNSUPPORTED;
     RotaryParams p = {};
     rows_in(p.x, x, x_strides, H);
     rows_out(p.x, out, out_strides);
@@ -284,7 +283,7 @@ int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const i
     if (rc != VECINFER_OK) return rc;
     if (B < 1 || N < 1 || max_pages < 1 || num_q_heads < 1 || num_q_heads % pages->num_kv_heads) return VECINFER_EINVAL;
     if ((N + pages->page_size - 1) / pages->page_size > max_pages) return VECINFER_EINVAL;
-    if (num_splits < 0 || num_splits > VECINFER_MAX_SPLITS || !isfinite(scale)) return VECINFER_EINVAL;
+    if (num_splits < 0 || num_splits > VECINFER_MAX_SPLITS || !isfinite(scale * kLog2e)) return VECINFER_EINVAL;
     if (!aligned(q, 16) || !aligned(out, 16) || !strides_ok(q_strides, 2, kStride)) return VECINFER_EINVAL;
     if (!aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(lse, 4) || !aligned(weights_in, 4) || !aligned(weights_out, 4))
         return VECINFER_EINVAL;

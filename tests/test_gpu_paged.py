@@ -406,3 +406,82 @@ def test_batches_dealt_by_length(B, Hq, Hkv, D, N, how):
             "none": torch.zeros(B)}[how].int().tolist()
     w = torch.rand(B, Hkv, N, generator=g).cuda() if B < 20 else None
     attend(c, c.queries(Hq), lens, weights=w)
+
+
+def test_dealt_batches_in_any_workspace():
+    c = Cache(3, 2, 64, 64, 5000)
+    q, lens = c.queries(8), [5000, 17, 1234]
+    least, most = (vb.vecinfer_paged_workspace_bytes(c.pages, 8, 3, 5000, s) for s in (1, 0))
+    for size in (least, (least + most) // 2 // 256 * 256, most):
+        attend(c, q, lens, ws=torch.full((size,), 255, dtype=torch.uint8, device="cuda"))
+
+
+def test_dealt_batches_in_a_graph():
+    """Lengths that change between the replays."""
+    c = Cache(4, 2, 64, 64, 4500)
+    q, table, ws = c.queries(8), c.table.cuda(), vb.new_paged_workspace(c.pages, 8, 4, 4500, weights=1)
+    lens = torch.tensor([4500, 3, 900, 0], dtype=torch.int32, device="cuda")
+    out, w = torch.empty(4, 8, 64, dtype=c.dtype, device="cuda"), torch.zeros(4, 2, 4500, device="cuda")
+    call = lambda o, s: vb.vecinfer_paged_attention(c.pages, q, table, ws, o, seq_lens=lens, N=4500, weights_out=s)  # noqa: E731
+    call(out, w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out, w)
+    for new in ([4500, 3, 900, 0], [1, 4500, 4500, 4500], [0, 0, 0, 0], [700, 4000, 2, 4499]):
+        lens.copy_(torch.tensor(new, dtype=torch.int32))
+        w.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager, sums = torch.empty_like(out), torch.zeros_like(w)
+        call(eager, sums)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(w, sums)
+        want = ref.attention(q.cpu(), c.k.cpu(), c.v.cpu(), c.table, new, 0.125)
+        ref.close(out, want["out"], want["tol_out"] + ref.half_step(want["out"].abs() + want["tol_out"], c.dtype), "out")
+
+
+def test_two_streams_at_once():
+    """Two calls with workspaces of their own, at the same time."""
+    cs = [Cache(2, 2, 128, 16, 3000, seed=i) for i in range(2)]
+    qs = [c.queries(8) for c in cs]
+    want = [attend(c, q)[0] for c, q in zip(cs, qs)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty_like(want[0]) for _ in range(20)] for _ in range(2)]
+    wss, tables = [vb.new_paged_workspace(c.pages, 8, 2, 3000) for c in cs], [c.table.cuda() for c in cs]
+    torch.cuda.synchronize()
+    for turn in range(20):
+        for i in range(2):
+            vb.vecinfer_paged_attention(cs[i].pages, qs[i], tables[i], wss[i], outs[i][turn], N=3000, stream=streams[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i in range(2) for o in outs[i])
+
+
+def test_both_ways_into_the_library(monkeypatch):
+    """The native argument checks and the interpreter's make the same calls."""
+    c = Cache(2, 2, 64, 16, 200, "bf16")
+    q = torch.randn(2, 9, 4, 64, generator=c.g).to(c.dtype).cuda()[:, 3]
+    table, lens = c.table.cuda(), torch.tensor([200, 77], dtype=torch.int32, device="cuda")
+    rot = vb.Rotary(64, 32, 1)
+    rt = vb.new_rotary_table(rot)
+    kn = torch.randn(2, 3, 2, 64, generator=c.g).to(c.dtype).cuda().transpose(1, 2)
+
+    def everything():
+        pages = vb.Pages(c.k.clone(), c.v.clone())
+        out, lse, w = torch.empty(2, 4, 64, dtype=c.dtype, device="cuda"), torch.empty(2, 4, device="cuda"), torch.ones(2, 2, 200, device="cuda")
+        qo = torch.zeros(2, 2, 3, 64, dtype=c.dtype, device="cuda")
+        vb.vecinfer_paged_append(pages, kn, kn, table, lens, rot=rot, table=rt, q=kn, q_out=qo, weights=w)
+        vb.vecinfer_paged_attention(pages, q, table, vb.new_paged_workspace(pages, 4, 2, 200, weights=1), out, lse=lse, seq_lens=lens, N=200,
+                                    scale=0.3, weights_in=w, weights_out=w)
+        dst, dl = vb.Pages(torch.zeros_like(c.k), torch.zeros_like(c.v)), torch.zeros(2, dtype=torch.int32, device="cuda")
+        dw, kept = torch.zeros(2, 2, 50, device="cuda"), torch.zeros(2, 2, 50, dtype=torch.int32, device="cuda")
+        vb.vecinfer_paged_evict(pages, w, table, dst, table, dl, vb.new_evict_workspace(pages, 2, 200, 50), 50, first=1, recent=5, seq_lens=lens,
+                                N=200, dst_weights=dw, kept=kept)
+        back = torch.empty_like(qo)
+        vb.vecinfer_rotary(rot, rt, qo, back, pos0=4, inverse=True)
+        torch.cuda.synchronize()
+        return pages.k, pages.v, out, lse, w, qo, dst.k, dst.v, dl, dw, kept, back
+
+    native = everything()
+    assert vb._fast is not None
+    monkeypatch.setattr(vb, "_fast", None)
+    assert all(torch.equal(a, b) for a, b in zip(native, everything()))

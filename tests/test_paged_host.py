@@ -29,7 +29,7 @@ def pages(**change):
 BAD_ROTARY = [(dict(head_dim=96), EUNSUP), (dict(rot_dim=0), EUNSUP), (dict(rot_dim=24), EUNSUP), (dict(rot_dim=144), EUNSUP),
               (dict(head_dim=64), EUNSUP), (dict(interleaved=2), EINVAL), (dict(scaling=4), EINVAL), (dict(scaling=-1), EINVAL),
               (dict(base=0.0), EINVAL), (dict(base=float("nan")), EINVAL), (dict(base=float("inf")), EINVAL),
-              (dict(magnitude=float("nan")), EINVAL), (dict(scaling=1, factor=0.0), EINVAL), (dict(scaling=2, factor=float("inf")), EINVAL),
+              (dict(magnitude=float("nan")), EINVAL), (dict(magnitude=1e39), EINVAL), (dict(scaling=1, factor=0.0), EINVAL), (dict(scaling=2, factor=float("inf")), EINVAL),
               (dict(scaling=3, factor=2.0, low_turns=4.0), EINVAL), (dict(scaling=3, factor=2.0, orig_len=0), EINVAL),
               (dict(scaling=3, factor=2.0, high_turns=float("inf")), EINVAL)]
 BAD_PAGES = [(dict(k=None), EINVAL), (dict(v=FAKE + 8), EINVAL), (dict(dtype=2), EINVAL), (dict(head_dim=96), EUNSUP),
@@ -64,7 +64,7 @@ def call_rotary(**change):
     (dict(cfg=None), EINVAL), (dict(table=None), EINVAL), (dict(x=None), EINVAL), (dict(out=None), EINVAL), (dict(xs=None), EINVAL),
     (dict(os=None), EINVAL), (dict(dtype=2), EINVAL), (dict(dtype=-1), EINVAL), (dict(B=0), EINVAL), (dict(H=0), EINVAL), (dict(T=0), EINVAL),
     (dict(T=-1), EINVAL), (dict(x=FAKE + 2), EINVAL), (dict(out=FAKE + 8), EINVAL), (dict(positions=FAKE + 2), EINVAL),
-    (dict(xs=S3(0, 0, 7)), EINVAL), (dict(xs=S3(0, -8, 8)), EINVAL), (dict(os=S3(0, 1 << 41, 8)), EINVAL), (dict(T=1 << 30), EUNSUP)])
+    (dict(xs=S3(0, 0, 7)), EINVAL), (dict(xs=S3(0, -8, 8)), EINVAL), (dict(os=S3(0, 1 << 41, 8)), EINVAL), (dict(T=1 << 30), EUNSUP), (dict(H=65536), EUNSUP)])
 def test_rotary_refuses(change, code):
     assert call_rotary(**change) == code
 
@@ -113,10 +113,10 @@ def call_attention(**change):
     (dict(pages=None), EINVAL), (dict(q=None), EINVAL), (dict(qs=None), EINVAL), (dict(bt=None), EINVAL), (dict(out=None), EINVAL),
     (dict(Hq=0), EINVAL), (dict(Hq=12), EINVAL), (dict(Hq=8 * 17), EUNSUP), (dict(B=0), EINVAL), (dict(B=70000), EUNSUP), (dict(N=0), EINVAL),
     (dict(N=161), EINVAL), (dict(mp=0), EINVAL), (dict(S=-1), EINVAL), (dict(S=257), EINVAL), (dict(scale=float("nan")), EINVAL),
-    (dict(scale=float("inf")), EINVAL), (dict(q=FAKE + 8), EINVAL), (dict(out=FAKE + 2), EINVAL), (dict(qs=(C.c_int64 * 2)(8, 4)), EINVAL),
+    (dict(scale=float("inf")), EINVAL), (dict(scale=3e38), EINVAL), (dict(q=FAKE + 8), EINVAL), (dict(out=FAKE + 2), EINVAL), (dict(qs=(C.c_int64 * 2)(8, 4)), EINVAL),
     (dict(bt=FAKE + 2), EINVAL), (dict(lens=FAKE + 2), EINVAL), (dict(lse=FAKE + 2), EINVAL), (dict(wi=FAKE, w_cap=200), EINVAL),
     (dict(wo=FAKE, w_cap=149), EINVAL), (dict(wo=FAKE + 1, w_cap=200), EINVAL), (dict(ws=None), EWORK), (dict(ws=FAKE + 16), EWORK),
-    (dict(wb=0), EWORK), (dict(S=4, wb=1 << 10), EWORK), (dict(N=(1 << 30) + 1, mp=1 << 40), EUNSUP)])
+    (dict(wb=0), EWORK), (dict(S=4, wb=1 << 10), EWORK), (dict(N=(1 << 30) + 1, mp=1 << 30), EUNSUP), (dict(mp=1 << 31), EUNSUP)])
 def test_attention_refuses(change, code):
     assert call_attention(**change) == code
 
