@@ -10,7 +10,7 @@
 // for short rows the steps themselves (500 tokens 7 us, 8192 9.8, 32000 22).  So a row of up to kHeld tokens, whose keys fit
 // a workgroup's registers, is one workgroup's in one launch, and a longer one is cut into up to kMaxParts stretches, a launch
 // per digit and one for the list, through a histogram per stretch: each workgroup of the next launch adds them up for
-// itself, which needs no atomics, no clearing and no order of workgroups (100003 tokens: 27 us in four launches; by one
+// itself, which needs no atomics, no clearing and no order of workgroups (100003 tokens: 24 us in four launches; by one
 // workgroup, the row read again for each digit, 89).
 // The move: 16 lanes per row of a kept token, keys and values; bound by memory (32768 of 100003 tokens, 8 KV heads, 268 MB:
 // 52 us, the rate of a large copy).
@@ -28,7 +28,7 @@ constexpr int kCopies = 4;                                // of a histogram in L
 // sequence of 20000 tokens, 8 KV heads, keeping 2000: 24.2 us by a workgroup per row, 33.3 shared; 32000 30.3 and 33.6).
 constexpr int kTurnsWhole = 8, kTurnsPart = 4;
 constexpr int kHeld = kSelect * 4 * kTurnsWhole, kHeldPart = kSelect * 4 * kTurnsPart;
-constexpr int kPart = kHeldPart / 2;                      // tokens of a stretch, unless that makes too many
+constexpr int kPart = kHeldPart / 4;                      // least tokens of a stretch
 constexpr int kMaxParts = 64;
 constexpr int kGroup = 32, kGroups = kBins / kGroup, kHist = kBins + kGroups;    // a stretch's histogram in memory
 
@@ -431,12 +431,16 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p)
 
 } // namespace
 
-// Workgroups that share a row in the choice.
+// Workgroups that share a row in the choice: as many as fill the chip once, of 4096 tokens at least and 16384, whose keys
+// are held, at most (8 rows, us of the whole call at 48000 / 100003 / 196000 tokens: stretches of 4096 35.5 / 78.4 / 47.3, of
+// 8192 38.0 / 81.0 / 39.8, of 16384 44.9 / 87.1 / 45.6; at 196000 stretches of 4096 are 384 workgroups).
 int evict_parts(long long rows, long long N)
 {
     if (N <= kHeld) return 1;
-    long long parts = (N + kPart - 1) / kPart;
-    if (rows * parts > 4 * num_cus()) parts = (N + kHeldPart - 1) / kHeldPart;     // the rows alone fill the chip
+    long long parts = num_cus() / rows;
+    const long long most = (N + kPart - 1) / kPart, least = (N + kHeldPart - 1) / kHeldPart;
+    if (parts > most) parts = most;
+    if (parts < least) parts = least;
     return (int)(parts < kMaxParts ? parts : kMaxParts);
 }
 
