@@ -177,7 +177,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
     const int g = blockIdx.y;
     int b, S, n0, n1;                                     // this workgroup's sequence, its splits, the tokens [n0, n1)
     size_t first, part;                                   // partial of its split 0, and its own
-    if constexpr (!DEALT) {                                 // every sequence in as many splits
+    if constexpr (!DEALT) {                               // every sequence in as many splits
         const int split = blockIdx.x;
         b = blockIdx.z;
         S = parts;
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
             chunk = chunk < (unsigned)p.least ? (unsigned)p.least : chunk;
             pieces = lane < B ? (own > chunk ? (own + chunk - 1) / chunk : 1u) : 0u;
             upto = wave_upto(pieces);
-            if (__builtin_amdgcn_readlane(upto, 63) <= (unsigned)parts) break;
+            if ((unsigned)__builtin_amdgcn_readlane(upto, 63) <= (unsigned)parts) break;
         }
         const unsigned long long mine = __ballot(blockIdx.x < upto);
         if (mine == 0) return;                            // fewer splits than workgroups

@@ -485,3 +485,23 @@ def test_both_ways_into_the_library(monkeypatch):
     assert vb._fast is not None
     monkeypatch.setattr(vb, "_fast", None)
     assert all(torch.equal(a, b) for a, b in zip(native, everything()))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_another_device_is_refused(monkeypatch, native):
+    """Tensors that are not on the current device: an error, and nothing is enqueued."""
+    c = Cache(1, 2, 64, 16, 64)
+    q, table, out = c.queries(4), c.table.cuda(), torch.full((1, 4, 64), 7.0, dtype=c.dtype, device="cuda")
+    ws, rot = vb.new_paged_workspace(c.pages, 4, 1, 64), vb.Rotary(64, 64)
+    rt, x = vb.new_rotary_table(rot), torch.ones(1, 2, 3, 64, dtype=c.dtype, device="cuda")
+    lens = torch.tensor([3], dtype=torch.int32, device="cuda")
+    if not native:
+        monkeypatch.setattr(vb, "_fast", None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: vb.vecinfer_paged_attention(c.pages, q, table, ws, out), lambda: vb.vecinfer_rotary(rot, rt, x, x),
+                 lambda: vb.vecinfer_paged_append(c.pages, x, x, table, lens)):
+        with pytest.raises(ValueError):
+            call()
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert (out == 7).all() and (x == 1).all()
