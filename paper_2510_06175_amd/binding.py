@@ -288,7 +288,8 @@ def _bind_fast(L: C.CDLL) -> None:
         m.bind(*(C.cast(getattr(L, "vecinfer_" + n), C.c_void_p).value for n in (
             "encode_keys", "encode_values", "append_kv", "decode_attention", "decode_attention_residual", "decode_step")), _stream)
         m.bind_paged(*(C.cast(getattr(L, "vecinfer_" + n), C.c_void_p).value for n in (
-            "rotary", "paged_append", "paged_attention", "paged_evict")), _stream_on)
+            "rotary", "paged_append", "paged_attention", "paged_evict")), _stream_on,
+                     getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None))
         _fast = m
 
 

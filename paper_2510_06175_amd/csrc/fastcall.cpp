@@ -33,6 +33,7 @@ decltype(&vecinfer_paged_attention) paged_attention_call;
 decltype(&vecinfer_paged_evict) paged_evict_call;
 PyObject *find_stream;                   // binding._stream
 PyObject *find_stream_on;                // binding._stream_on
+PyObject *get_device, *get_stream;       // torch's own functions for the current device and its stream's handle, or None
 
 struct Refused {};                       // an argument that the interpreter's checks have to look at
 struct Raised {};                        // Python's error is set
@@ -304,9 +305,24 @@ void *rows(const at::Tensor &t, int64_t device, at::ScalarType type, std::initia
     return t.data_ptr();
 }
 
-// The stream for work on that device; raises where it is not the current one.
+// The stream for work on that device; raises where it is not the current one.  The usual case, the current stream of the
+// current device, is asked of torch's own functions (0.2 us less than by binding._stream_on, of 4 for a small call).
 void *stream_on(PyObject *o, int64_t device)
 {
+    if (o == Py_None && get_device != Py_None && get_stream != Py_None) {
+        PyObject *const d = PyObject_CallNoArgs(get_device);
+        if (!d) throw Raised();
+        const bool current = PyLong_CheckExact(d) && PyLong_AsLongLong(d) == device;
+        PyObject *const s = current ? PyObject_CallOneArg(get_stream, d) : nullptr;
+        Py_DECREF(d);
+        if (current) {
+            if (!s) throw Raised();
+            void *const p = PyLong_Check(s) ? PyLong_AsVoidPtr(s) : nullptr;
+            Py_DECREF(s);
+            if (PyErr_Occurred()) throw Raised();
+            return p;
+        }
+    }
     PyObject *const dev = PyLong_FromLongLong(device);
     if (!dev) throw Raised();
     PyObject *const r = PyObject_CallFunctionObjArgs(find_stream_on, o, dev, nullptr);
@@ -462,11 +478,12 @@ PyObject *paged_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// bind_paged(addresses of the library's functions, in the order of the variables above, then the function for streams)
+// bind_paged(addresses of the library's functions, in the order of the variables above, then the function for streams and
+// torch's for the current device and for its stream's handle, or None)
 PyObject *bind_paged(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 5) {
-        PyErr_SetString(PyExc_TypeError, "bind_paged: four addresses and a function");
+    if (n != 7) {
+        PyErr_SetString(PyExc_TypeError, "bind_paged: four addresses and three functions");
         return nullptr;
     }
     void *p[4];
@@ -474,9 +491,12 @@ PyObject *bind_paged(PyObject *, PyObject *const *a, Py_ssize_t n)
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
-    Py_INCREF(a[4]);
-    Py_XDECREF(find_stream_on);
-    find_stream_on = a[4];
+    PyObject **const held[3] = {&find_stream_on, &get_device, &get_stream};
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(a[4 + i]);
+        Py_XDECREF(*held[i]);
+        *held[i] = a[4 + i];
+    }
     rotary_call = reinterpret_cast<decltype(rotary_call)>(p[0]);
     paged_append_call = reinterpret_cast<decltype(paged_append_call)>(p[1]);
     paged_attention_call = reinterpret_cast<decltype(paged_attention_call)>(p[2]);

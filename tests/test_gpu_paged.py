@@ -495,13 +495,17 @@ def test_another_device_is_refused(monkeypatch, native):
     ws, rot = vb.new_paged_workspace(c.pages, 4, 1, 64), vb.Rotary(64, 64)
     rt, x = vb.new_rotary_table(rot), torch.ones(1, 2, 3, 64, dtype=c.dtype, device="cuda")
     lens = torch.tensor([3], dtype=torch.int32, device="cuda")
-    if not native:
-        monkeypatch.setattr(vb, "_fast", None)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    if native:
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+        vb._bind_fast(vb.lib())
+    else:
+        monkeypatch.setattr(vb, "_fast", None)
     for call in (lambda: vb.vecinfer_paged_attention(c.pages, q, table, ws, out), lambda: vb.vecinfer_rotary(rot, rt, x, x),
                  lambda: vb.vecinfer_paged_append(c.pages, x, x, table, lens)):
         with pytest.raises(ValueError):
             call()
     monkeypatch.undo()
+    vb._bind_fast(vb.lib())
     torch.cuda.synchronize()
     assert (out == 7).all() and (x == 1).all()
