@@ -34,7 +34,9 @@ template <typename E> struct Vec;
 template <> struct Vec<f16> {
     typedef f16 v8 __attribute__((ext_vector_type(8)));
     static __device__ __forceinline__ floatx4 mfma(v8 a, v8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-    // Probabilities are held times 2^15: fp16 then has them in full down to 2^-29 of the largest.
+    // Probabilities, and so their sums and outputs in front of the division, are held times 2^15: fp16 then has them in full
+    // down to 2^-29 of the largest.  The lift goes onto a score's distance from the maximum, never onto the maximum, from
+    // which fp32 cannot take 15 where it is 2^24 and more (and 2^16, as which 1 was held there, is no fp16 number).
     static constexpr float kLift = 15.f;
 };
 template <> struct Vec<bf16> {
@@ -119,7 +121,7 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, arr
         }
         den = wave_all(den, [](float a, float b) { return a + b; });
         if (lane == 0) {
-            const float total = den == 0.f ? -INFINITY : M + log2f(den);
+            const float total = den == 0.f ? -INFINITY : M + (log2f(den) - Vec<E>::kLift);
             den_s[h] = den;
             if (p.lse) p.lse[row0 + h] = natural(total);
             if (p.lse2) p.lse2[row0 + h] = total;
@@ -338,11 +340,11 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
 #pragma unroll
             for (int i = 0; i < kVE; ++i) acc[i] *= f;
         }
-        const float base = (m > -INFINITY ? m : 0.f) - Vec<E>::kLift;
+        const float base = m > -INFINITY ? m : 0.f;
         vec8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float x = __builtin_amdgcn_exp2f(s[e] - base);
+            const float below = s[e] - base, x = __builtin_amdgcn_exp2f(Vec<E>::kLift > 0.f ? below + Vec<E>::kLift : below);
             l += x;
             hi[e] = (E)x;
             lo[e] = (E)(x - (float)hi[e]);
@@ -399,7 +401,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
         if (S == 1) {
             static_cast<E *>(p.out)[(row0 + h) * D + ch] = (E)(den == 0.f ? 0.f : o / den);
             if (ch == 0) {
-                const float total = den == 0.f ? -INFINITY : M - Vec<E>::kLift + log2f(den);
+                const float total = den == 0.f ? -INFINITY : M + (log2f(den) - Vec<E>::kLift);
                 if (p.lse) p.lse[row0 + h] = natural(total);
                 if (p.lse2) p.lse2[row0 + h] = total;
             }
@@ -407,7 +409,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
             const size_t at_s = part * G + h;
             shared_store(p.part_o + at_s * D + ch, o);
             if (ch == 0) {
-                shared_store(p.part_m + at_s, M - Vec<E>::kLift);
+                shared_store(p.part_m + at_s, M);
                 shared_store(p.part_l + at_s, den);
             }
         }

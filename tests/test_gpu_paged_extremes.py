@@ -1,0 +1,83 @@
+"""Paged decode attention on the GPU where scores are very large, against the formula in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_reference as ref
+from paper_2510_06175_amd import binding as vb
+from test_gpu_paged import Cache, attend
+
+pytestmark = pytest.mark.gpu
+
+
+def unit_scale():
+    """A softmax scale that is one in the units of the scores' powers of two: scale * log2(e) = 1 in fp32."""
+    x = np.float32(math.log(2))
+    for s in (x, np.nextafter(x, np.float32(0)), np.nextafter(x, np.float32(1))):
+        if s * np.float32(math.log2(math.e)) == 1:
+            return float(s)
+    raise AssertionError("no such scale")
+
+
+def far_scores(j, sign, dtype, lens, N=300):
+    """A cache and queries (64 channels, two query heads per KV head) whose scores are sign 2^j + step n in powers of two, n = 0 .. 3
+    by the token and step the spacing of fp32 numbers there, or 1.  All products and sums of a score are exact in fp32, so the
+    probabilities 2^(score - largest) are known.  Returns the cache, the queries and, per sequence, the probabilities [Hkv, n] and the
+    logarithm of the sum."""
+    c = Cache(len(lens), 2, 64, 16, N, dtype, seed=j)
+    step = max(1.0, 2.0 ** (j - 23))
+    q = torch.zeros(len(lens), 4, 64)
+    q[..., 0], q[..., 1] = 2.0 ** 15, sign * step
+    n = torch.randint(0, 4, c.k.shape[:3], generator=c.g)
+    k = torch.zeros(c.k.shape)
+    k[..., 0], k[..., 1] = sign * 2.0 ** (j - 15), n.float()
+    c.k.copy_(k)
+    want = []
+    for b, m in enumerate(lens):
+        rows, _ = ref.gather(k, c.table[b], m, 16)
+        d = (rows * q[b, 0].double()).sum(-1)
+        top = d.amax(-1, keepdim=True)
+        e = torch.exp2(d - top)
+        want.append((e / e.sum(-1, keepdim=True), (top[:, 0] + torch.log2(e.sum(-1))) * math.log(2)))
+    return c, q.to(c.dtype).cuda(), want
+
+
+# of the probabilities and their sums, relative: as in paged_reference.attention
+def rest(n, dtype):
+    return (n + 64) * 2.0 ** -23 + 2.0 ** -20 + (2.0 ** -17 if dtype == "bf16" else 2.0 ** -22)
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("j", [10, 20, 22, 23, 24, 25, 26, 27, 28, 29, 30])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_scores_of_every_size(dtype, sign, j, splits):
+    """Probabilities do not depend on how large the scores are, as long as fp32 has their differences."""
+    lens = [300, 37]
+    c, q, want = far_scores(j, sign, dtype, lens)
+    out, lse, _ = attend(c, q, lens, splits=splits, scale=unit_scale(), check=False)
+    for b, n in enumerate(lens):
+        p, total = want[b]
+        v, _ = ref.gather(c.v.cpu(), c.table[b], n, 16)
+        for h in range(4):
+            o, tol = p[h // 2] @ v[h // 2], (p[h // 2] @ v[h // 2].abs()) * rest(n, dtype)
+            ref.close(out[b, h], o, tol + ref.half_step(o.abs() + tol, c.dtype), f"head {h}")
+            ref.close(lse[b, h], total[h // 2], rest(n, dtype) + 2.0 ** -21 * total[h // 2].abs(), "lse")
+
+
+@pytest.mark.parametrize("splits", [0, 1, 4])
+def test_rows_of_a_thousand(splits):
+    """Finite rows whose scores pass 2^24 at the usual scale: the tokens alike share the weight, their opposites have none."""
+    c = Cache(1, 1, 128, 16, 400, "fp16")
+    c.k[...] = 1100.0
+    last = c.table[0, -4:].long()
+    c.k[last.cuda()] = -1100.0
+    q = torch.full((1, 4, 128), 1100.0, dtype=c.dtype, device="cuda")
+    for sign, tokens in ((1.0, slice(0, 336)), (-1.0, slice(336, 400))):
+        out, _, _ = attend(c, sign * q, splits=splits, check=False)
+        v = ref.gather(c.v.cpu(), c.table[0], 400, 16)[0][0, tokens]
+        tol = v.abs().mean(0) * rest(400, "fp16")
+        for h in range(4):
+            ref.close(out[0, h], v.mean(0), tol + ref.half_step(v.mean(0).abs() + tol, c.dtype), f"sign {sign} head {h}")
