@@ -520,7 +520,9 @@ size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q
  *   s_t = scale q . k_t  over t < len_b that are not in a hole;   o = softmax(s) v;   L = log sum_t exp(s_t)
  * per (b, query head h), KV head h / G, G = H_q / H_kv in 1 .. 16.  Products and sums in fp32, one rounding of
  * the output.  Without a token to attend to (or with scores of -inf alone) o = 0 and L = -inf.  What the rows
- * behind a sequence's end hold is of no account, infinities and NaN included.
+ * behind a sequence's end hold is of no account, infinities and NaN included.  An infinite value of an attended
+ * token makes its channel of the output infinite, however little the token weighs (two of opposite signs, or a
+ * NaN, make it NaN).  Sums are divided last: bf16 values have to stay below 2^96.
  *   q          [B, H_q, D] by strides {b, h}             out  [B, H_q, D], contiguous, of the pages' type
  *   seq_lens   int32 [B] or NULL: N tokens each; clamped to [0, N]
  *   N          1 <= N <= max_pages page_size, N <= 2^30

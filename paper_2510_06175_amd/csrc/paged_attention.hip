@@ -38,12 +38,26 @@ template <> struct Vec<f16> {
     // down to 2^-29 of the largest.  The lift goes onto a score's distance from the maximum, never onto the maximum, from
     // which fp32 cannot take 15 where it is 2^24 and more (and 2^16, as which 1 was held there, is no fp16 number).
     static constexpr float kLift = 15.f;
+    static constexpr unsigned kInf = 0x7c00u;
 };
 template <> struct Vec<bf16> {
     typedef bf16 v8 __attribute__((ext_vector_type(8)));
     static __device__ __forceinline__ floatx4 mfma(v8 a, v8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static constexpr float kLift = 0.f;
+    static constexpr unsigned kInf = 0x7f80u;
 };
+
+// Weight of what has maximum m where the whole has maximum `all`.  Never 0, so that an infinite output stays one: with a
+// maximum of -inf, or a far lower one, what it weighs is 0 or as good as that.
+__device__ __forceinline__ float weight_of(float m, float all) { return fmaxf(__builtin_amdgcn_exp2f(m - all), 0x1p-126f); }
+
+// The infinite ones of two halves, 0 in place of the others.
+template <typename E>
+__device__ __forceinline__ unsigned infinite_halves(unsigned x)
+{
+    const unsigned low = (x & 0x7fffu) == Vec<E>::kInf ? 0xffffu : 0u, high = (x & 0x7fff0000u) == Vec<E>::kInf << 16 ? 0xffff0000u : 0u;
+    return x & (low | high);
+}
 
 // sum over the four 16-lane rows of the wavefront
 __device__ __forceinline__ float rows_sum(float x)
@@ -92,7 +106,7 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, arr
             for (int j = j0; j < j0 + kStep; ++j)
 #pragma unroll
                 for (int i = 0; i < kElems; ++i) {
-                    // (behind the last split, that one again at weight 0; behind the last element, the first)
+                    // (behind the last split, that one again, at the least weight there is; behind the last element, the first)
                     const int e = t + i * kBlock < GD ? t + i * kBlock : 0;
                     v[i][j] = shared_load(po + (size_t)(s0 + j < S ? s0 + j : S - 1) * GD + e);
                 }
@@ -112,10 +126,10 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, arr
 #pragma unroll
         for (int i = 0; i < kMergeSplits / 64; ++i) M = fmaxf(M, m[i]);
         M = wave_all(M, [](float a, float b) { return fmaxf(a, b); });
-        const float at = M > -INFINITY ? M : 0.f;         // nothing to attend to: all weights 0
+        const float at = M > -INFINITY ? M : 0.f;         // nothing to attend to: sums and outputs of 0 at any weight
 #pragma unroll
         for (int i = 0; i < kMergeSplits / 64; ++i) {
-            const float w = __builtin_amdgcn_exp2f(m[i] - at);
+            const float w = weight_of(m[i], at);
             wt_s[h * kMergeSplits + lane + 64 * i] = w;
             den = fmaf(w, l[i], den);
         }
@@ -231,136 +245,173 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
     const int last_col = (N - 1) >> shift;
     if (!DEALT && wave == 0 && 32 * lane <= last_col) (void)*const_cast<const volatile int32_t *>(pages + 32 * lane);
 
-    vec8 qf[kSteps];
-    {
-        const unsigned head = c < G ? ~0u : 0u;            // spare columns: zeros (by a mask: the request is not to wait for a branch)
-        const char *const row = q + b * p.q_b + (long long)(g * G + (c < G ? c : 0)) * p.q_h;
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j) {
-            const uint4 x = reinterpret_cast<const uint4 *>(row)[4 * j + kg];
-            qf[j] = as_vec<E>(x.x & head, x.y & head, x.z & head, x.w & head);
-        }
-    }
-
     const unsigned slot_mask = (1u << shift) - 1;
     const char *const k0 = k_pool + (size_t)g * p.pages.k_head, *const v0 = v_pool + (size_t)g * p.pages.v_head;
-    const int krow = 8 * (c >> 2) + (c & 3);              // this lane's key token of sub-tile 0; of sub-tile 1: + 4
     auto page_at = [&](int tok) {
         const int col = tok >> shift;
         return pages[col < last_col ? col : last_col];
     };
 
-    float m = -INFINITY, l = 0.f;
+    float m, l;
     floatx4 acc[kVE];
-#pragma unroll
-    for (int i = 0; i < kVE; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    // Keys and values of the next tile are requested as soon as this one's have been used, its pages a tile before that
-    // (196608 tokens, 32 / 8 heads: 142 us with all requests at the tile's start, 139 so).  Values are not to be kept in any
-    // cache: 125.  Keys are: a request takes 64 bytes of each row, half a cache line, and the next one the other half (without
-    // caching 129 us, and a workgroup by itself a quarter slower).
-    uint4 kr[2][kSteps];
-    unsigned vr[8][kVW];
-    auto load_k = [&](int t0, unsigned page) {
-        const char *row = k0 + (size_t)(page < p.pages.num_pages ? page : 0u) * p.pages.k_page +
-                          (size_t)((unsigned)(t0 + krow) & slot_mask) * p.pages.k_slot + 16 * kg;
+    // The tiles of this wavefront, whose lane this is; `apart`: with infinite values taken out and added by themselves.
+    auto tiles = [&](auto apart, int lane) {
+        const int kg = lane >> 4, c = lane & 15;
+        const int krow = 8 * (c >> 2) + (c & 3);          // this lane's key token of sub-tile 0; of sub-tile 1: + 4
+        vec8 qf[kSteps];
+        {
+            const unsigned head = c < G ? ~0u : 0u;       // spare columns: zeros (by a mask: the request is not to wait for a branch)
+            const char *const row = q + b * p.q_b + (long long)(g * G + (c < G ? c : 0)) * p.q_h;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j) kr[u][j] = *reinterpret_cast<const uint4 *>(row + 64 * j);
-            row += 4 * (size_t)p.pages.k_slot;
+            for (int j = 0; j < kSteps; ++j) {
+                const uint4 x = reinterpret_cast<const uint4 *>(row)[4 * j + kg];
+                qf[j] = as_vec<E>(x.x & head, x.y & head, x.z & head, x.w & head);
+            }
         }
-    };
-    auto load_v = [&](int t0, unsigned page) {
-        const char *row = v0 + (size_t)(page < p.pages.num_pages ? page : 0u) * p.pages.v_page +
-                          (size_t)((unsigned)(t0 + 8 * kg) & slot_mask) * p.pages.v_slot + 2 * kVE * c;
+        // Keys and values of the next tile are requested as soon as this one's have been used, its pages a tile before that
+        // (196608 tokens, 32 / 8 heads: 142 us with all requests at the tile's start, 139 so).  Values are not to be kept in any
+        // cache: 125.  Keys are: a request takes 64 bytes of each row, half a cache line, and the next one the other half (without
+        // caching 129 us, and a workgroup by itself a quarter slower).
+        uint4 kr[2][kSteps];
+        unsigned vr[8][kVW];
+        auto load_k = [&](int t0, unsigned page) {
+            const char *row = k0 + (size_t)(page < p.pages.num_pages ? page : 0u) * p.pages.k_page +
+                              (size_t)((unsigned)(t0 + krow) & slot_mask) * p.pages.k_slot + 16 * kg;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const words x = __builtin_nontemporal_load(reinterpret_cast<const words *>(row));
+            for (int u = 0; u < 2; ++u) {
 #pragma unroll
-            for (int w = 0; w < kVW; ++w) vr[j][w] = x[w];
-            row += p.pages.v_slot;
+                for (int j = 0; j < kSteps; ++j) kr[u][j] = *reinterpret_cast<const uint4 *>(row + 64 * j);
+                row += 4 * (size_t)p.pages.k_slot;
+            }
+        };
+        auto load_v = [&](int t0, unsigned page) {
+            const char *row = v0 + (size_t)(page < p.pages.num_pages ? page : 0u) * p.pages.v_page +
+                              (size_t)((unsigned)(t0 + 8 * kg) & slot_mask) * p.pages.v_slot + 2 * kVE * c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const words x = __builtin_nontemporal_load(reinterpret_cast<const words *>(row));
+#pragma unroll
+                for (int w = 0; w < kVW; ++w) vr[j][w] = x[w];
+                row += p.pages.v_slot;
+            }
+        };
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kVE; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        int t0 = n0 + wave * kTokens;
+        unsigned page_k = 0, page_v = 0;                  // of the tile in hand, then of the next
+        if (t0 < n1) {
+            page_k = (unsigned)page_at(t0 + krow);
+            page_v = (unsigned)page_at(t0 + 8 * kg);
+            load_k(t0, page_k);
+            load_v(t0, page_v);
         }
-    };
-    int t0 = n0 + wave * kTokens;
-    unsigned page_k = 0, page_v = 0;                      // of the tile in hand, then of the next
-    if (t0 < n1) {
-        page_k = (unsigned)page_at(t0 + krow);
-        page_v = (unsigned)page_at(t0 + 8 * kg);
-        load_k(t0, page_k);
-        load_v(t0, page_v);
-    }
-    while (t0 < n1) {
-        const bool there = page_v < p.pages.num_pages;
-        const int tn = t0 + NW * kTokens;
-        if (tn < n1) {
-            page_k = (unsigned)page_at(tn + krow);
-            page_v = (unsigned)page_at(tn + 8 * kg);
-        }
-        // ---- scores, in log2 units: head c, tokens t0 + 8 kg + e
-        float s[8];
+        while (t0 < n1) {
+            const bool there = page_v < p.pages.num_pages;
+            const int tn = t0 + NW * kTokens;
+            if (tn < n1) {
+                page_k = (unsigned)page_at(tn + krow);
+                page_v = (unsigned)page_at(tn + 8 * kg);
+            }
+            // ---- scores, in log2 units: head c, tokens t0 + 8 kg + e
+            float s[8];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            floatx4 d = {0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < 2; ++u) {
+                floatx4 d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) d = Vec<E>::mfma(__builtin_bit_cast(vec8, kr[u][j]), qf[j], d);
+                for (int j = 0; j < kSteps; ++j) d = Vec<E>::mfma(__builtin_bit_cast(vec8, kr[u][j]), qf[j], d);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[4 * u + r] = d[r] * p.scale2;
-        }
-        if (tn < n1) load_k(tn, page_k);
-        // A tile with a hole, or the sequence's last: what is not there has no score, and whatever its rows hold (an
-        // infinity times a probability of 0 is NaN) is taken out.
-        if (t0 + kTokens > n1 || !__all(there)) {
+                for (int r = 0; r < 4; ++r) s[4 * u + r] = d[r] * p.scale2;
+            }
+            if (tn < n1) load_k(tn, page_k);
+            // A tile with a hole, or the sequence's last: what is not there has no score, and whatever its rows hold (an
+            // infinity times a probability of 0 is NaN) is taken out.
+            if (t0 + kTokens > n1 || !__all(there)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool in = there && t0 + 8 * kg + e < n1;
+                    s[e] = in ? s[e] : -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < kVW; ++w) vr[e][w] = in ? vr[e][w] : 0u;
+                }
+            }
+            if constexpr (SCORES) {
+                if (c < G) {
+                    float *const to = p.scores + (row0 + c) * p.n_pad + t0 + 8 * kg;
+                    reinterpret_cast<float4 *>(to)[0] = make_float4(s[0], s[1], s[2], s[3]);
+                    reinterpret_cast<float4 *>(to)[1] = make_float4(s[4], s[5], s[6], s[7]);
+                }
+            }
+
+            // ---- softmax: every lane of a head has the same maximum, and a sum of its own tokens
+            float top = s[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
+            top = rows_max(top);
+            if (__any(top > m)) {
+                const float to = fmaxf(m, top);
+                const float f = weight_of(m, to);
+                m = to;
+                l *= f;
+#pragma unroll
+                for (int i = 0; i < kVE; ++i) acc[i] *= f;
+            }
+            const float base = m > -INFINITY ? m : 0.f;
+            vec8 hi, lo;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool in = there && t0 + 8 * kg + e < n1;
-                s[e] = in ? s[e] : -INFINITY;
-#pragma unroll
-                for (int w = 0; w < kVW; ++w) vr[e][w] = in ? vr[e][w] : 0u;
+                const float below = s[e] - base, x = __builtin_amdgcn_exp2f(Vec<E>::kLift > 0.f ? below + Vec<E>::kLift : below);
+                l += x;
+                hi[e] = (E)x;
+                lo[e] = (E)(x - (float)hi[e]);
             }
-        }
-        if constexpr (SCORES) {
-            if (c < G) {
-                float *const to = p.scores + (row0 + c) * p.n_pad + t0 + 8 * kg;
-                reinterpret_cast<float4 *>(to)[0] = make_float4(s[0], s[1], s[2], s[3]);
-                reinterpret_cast<float4 *>(to)[1] = make_float4(s[4], s[5], s[6], s[7]);
+
+            // ---- output
+            auto turned = [&](const unsigned(&x)[8][kVW], int i) {
+                const unsigned pick = i & 1 ? 0x07060302u : 0x05040100u;   // high or low halves of two rows' words
+                return as_vec<E>(__builtin_amdgcn_perm(x[1][i / 2], x[0][i / 2], pick), __builtin_amdgcn_perm(x[3][i / 2], x[2][i / 2], pick),
+                                 __builtin_amdgcn_perm(x[5][i / 2], x[4][i / 2], pick), __builtin_amdgcn_perm(x[7][i / 2], x[6][i / 2], pick));
+            };
+            if constexpr (decltype(apart)::value) {
+                vec8 scored;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) scored[e] = (E)(s[e] > -INFINITY ? 1.f : 0.f);
+#pragma unroll
+                for (int i = 0; i < kVE; ++i) {
+                    const uintx4 a = __builtin_bit_cast(uintx4, turned(vr, i));
+                    uintx4 inf;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) inf[w] = infinite_halves<E>(a[w]);
+                    acc[i] = Vec<E>::mfma(__builtin_bit_cast(vec8, inf), scored, acc[i]);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int w = 0; w < kVW; ++w) vr[e][w] &= ~infinite_halves<E>(vr[e][w]);
             }
-        }
-
-        // ---- softmax: every lane of a head has the same maximum, and a sum of its own tokens
-        float top = s[0];
 #pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
-        top = rows_max(top);
-        if (__any(top > m)) {
-            const float to = fmaxf(m, top);
-            const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(m - to) : 0.f;
-            m = to;
-            l *= f;
-#pragma unroll
-            for (int i = 0; i < kVE; ++i) acc[i] *= f;
+            for (int i = 0; i < kVE; ++i) {
+                const vec8 a = turned(vr, i);
+                acc[i] = Vec<E>::mfma(a, hi, acc[i]);
+                acc[i] = Vec<E>::mfma(a, lo, acc[i]);
+            }
+            if (tn < n1) load_v(tn, page_v);
+            t0 = tn;
         }
-        const float base = m > -INFINITY ? m : 0.f;
-        vec8 hi, lo;
+    };
+    tiles(std::false_type{}, lane);
+    // An infinite value belongs into the output, however little it weighs, but times probabilities in two parts, of which either
+    // may be 0 or negative, it makes no number.  A wavefront whose outputs are not all finite goes over its tiles once more, with
+    // the infinities apart, at weight 1.  (A sum of numbers of which one is not finite is not.)
+    floatx4 sum = acc[0];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float below = s[e] - base, x = __builtin_amdgcn_exp2f(Vec<E>::kLift > 0.f ? below + Vec<E>::kLift : below);
-            l += x;
-            hi[e] = (E)x;
-            lo[e] = (E)(x - (float)hi[e]);
-        }
-
-        // ---- output
-#pragma unroll
-        for (int i = 0; i < kVE; ++i) {
-            const unsigned pick = i & 1 ? 0x07060302u : 0x05040100u;       // high or low halves of two rows' words
-            vec8 a = as_vec<E>(__builtin_amdgcn_perm(vr[1][i / 2], vr[0][i / 2], pick), __builtin_amdgcn_perm(vr[3][i / 2], vr[2][i / 2], pick),
-                               __builtin_amdgcn_perm(vr[5][i / 2], vr[4][i / 2], pick), __builtin_amdgcn_perm(vr[7][i / 2], vr[6][i / 2], pick));
-            acc[i] = Vec<E>::mfma(a, hi, acc[i]);
-            acc[i] = Vec<E>::mfma(a, lo, acc[i]);
-        }
-        if (tn < n1) load_v(tn, page_v);
-        t0 = tn;
+    for (int i = 1; i < kVE; ++i) sum += acc[i];
+    if (__builtin_expect(!__all(fabsf((sum[0] + sum[1]) + (sum[2] + sum[3])) < INFINITY), false)) {
+        int again = lane;
+        asm volatile("" : "+v"(again));                   // (addresses that both shared would be worked out in front of the first)
+        tiles(std::true_type{}, again);
     }
 
     // ---- the wavefronts join
@@ -394,7 +445,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
         float den = 0.f, o = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float f = __builtin_amdgcn_exp2f(mw[w] - at);
+            const float f = weight_of(mw[w], at);
             den = fmaf(f, lw[w], den);
             o = fmaf(f, o_s[(w * KG + h) * D + ch], o);
         }

@@ -1,4 +1,4 @@
-"""Paged decode attention on the GPU where scores are very large, against the formula in 64 bits."""
+"""Paged decode attention on the GPU where scores are very large and values infinite, against the formula in 64 bits."""
 import math
 
 import numpy as np
@@ -81,3 +81,43 @@ def test_rows_of_a_thousand(splits):
         tol = v.abs().mean(0) * rest(400, "fp16")
         for h in range(4):
             ref.close(out[0, h], v.mean(0), tol + ref.half_step(v.mean(0).abs() + tol, c.dtype), f"sign {sign} head {h}")
+
+
+def whole_number_of(x):
+    """0 finite, 1 infinity, -1 its opposite, 2 not a number."""
+    return torch.where(torch.isnan(x), 2, torch.where(torch.isinf(x), torch.sign(x), 0)).int()
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,N,splits", [(1, 20, 1), (2, 500, 1), (2, 500, 3), (1, 700, 7), (1, 3000, 0), (3, 4100, 0)])
+@pytest.mark.parametrize("far", [False, True])
+def test_infinite_values(dtype, D, B, N, splits, far):
+    """An infinity among the attended values goes into its channel of its heads' outputs, however small its weight is, as in
+    the sum of the formula; two of opposite signs, or what is no number, give what is no number; other channels do not notice."""
+    c = Cache(B, 2, D, 16, N, dtype, seed=N)
+    lens = [N - 7 * b for b in range(B)]
+    q = c.queries(6, 2.0)
+    if far:                                       # (weights of 2^-400 and less for one half of the tokens, in channels of no other use)
+        c.k[..., 0] = torch.where(torch.arange(16, device="cuda") % 2 == 1, -30.0, 0.0).to(c.dtype)
+        q[..., 0] = 16.0
+    special = {3: (float("inf"),), 5: (float("-inf"),), 7: (float("inf"), float("-inf")), 11: (float("nan"),), 13: (float("inf"), float("inf"))}
+    clean = attend(c, q, lens, splits=splits, scale=1.0 if far else None)
+    want = {3: 1, 5: -1, 7: 2, 11: 2, 13: 1}
+    for at in (1, 9, 12, N // 2 + 1, N - 7 * B - (N - 7 * B) % 2):      # also among the last split's
+        if at < 0 or at >= min(lens):
+            continue
+        for b in range(B):
+            was = c.v.clone()
+            for ch, values in special.items():
+                for i, x in enumerate(values):
+                    t = max(0, at - 2 * i)
+                    c.v[int(c.table[b, t // 16]), 1, t % 16, ch] = x
+            out, lse, _ = attend(c, q, lens, splits=splits, scale=1.0 if far else None, check=False)
+            kind = torch.zeros(out.shape, dtype=torch.int32)
+            for ch in special:
+                kind[b, 3:, ch] = want[ch]
+            assert torch.equal(whole_number_of(out.cpu()), kind), (at, b)
+            assert torch.equal(lse, clean[1])
+            assert torch.equal(out.cpu()[kind == 0], clean[0].cpu()[kind == 0]), (at, b)
+            c.v.copy_(was)
