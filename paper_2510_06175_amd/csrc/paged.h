@@ -68,7 +68,7 @@ struct PagedParams {
     float *lse;                  // [B, Hq] or nullptr
     // sums of attention weight; scores == nullptr: none
     float *scores;               // [B, Hq, n_pad] scores in log2 units
-    float *lse2;                 // [B, Hq] log2 of the sum of exp2 of the scores
+    float2 *norm;                // [B, Hq]: weight = exp2(score - x) y, x the largest score, y 1 over the sum of these
     long long n_pad;
     const float *w_in;           // [B, Hkv, w_cap] or nullptr: 0
     float *w_out;                // [B, Hkv, w_cap]

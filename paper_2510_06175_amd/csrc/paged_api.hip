@@ -91,7 +91,7 @@ void rows_out(RowSet &r, void *x, const int64_t *s)
 }
 
 struct PagedLayout {
-    size_t off_o, off_m, off_l, off_words, off_lse2, off_scores, total;
+    size_t off_o, off_m, off_l, off_words, off_norm, off_scores, total;
 };
 
 // parts: partials of a (split, KV head) each
@@ -109,7 +109,7 @@ PagedLayout paged_layout(const vecinfer_pages *p, int32_t Hq, int32_t B, int64_t
     w.off_m = take(sizeof(float) * rows);
     w.off_l = take(sizeof(float) * rows);
     w.off_words = take(sizeof(unsigned long long) * kWordStep * (size_t)B * p->num_kv_heads);
-    w.off_lse2 = take(weights ? sizeof(float) * (size_t)B * Hq : 0);
+    w.off_norm = take(weights ? sizeof(float2) * (size_t)B * Hq : 0);
     w.off_scores = take(weights ? sizeof(float) * (size_t)B * Hq * ((N + 31) / 32 * 32) : 0);
     w.total = off;
     return w;
@@ -328,7 +328,7 @@ int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const i
     p.lse = lse;
     if (weights_out) {
         p.scores = reinterpret_cast<float *>(ws + w.off_scores);
-        p.lse2 = reinterpret_cast<float *>(ws + w.off_lse2);
+        p.norm = reinterpret_cast<float2 *>(ws + w.off_norm);
         p.n_pad = (N + 31) / 32 * 32;
         p.w_in = weights_in;
         p.w_out = weights_out;

@@ -51,6 +51,16 @@ template <> struct Vec<bf16> {
 // maximum of -inf, or a far lower one, what it weighs is 0 or as good as that.
 __device__ __forceinline__ float weight_of(float m, float all) { return fmaxf(__builtin_amdgcn_exp2f(m - all), 0x1p-126f); }
 
+// What takes a head's scores to weights: the maximum and 1 over the sum, not one number, whose rounding would be all weights'
+// (half a step of log2 of the sum is a factor of 2^0.5 at 2^23).
+template <typename E>
+__device__ __forceinline__ float2 norm_of(float at, float den)
+{
+    constexpr float lifted = Vec<E>::kLift > 0.f ? 0x1p15f : 1.f;
+    static_assert(Vec<E>::kLift == 0.f || Vec<E>::kLift == 15.f, "2^15");
+    return make_float2(at, den == 0.f ? 0.f : lifted / den);
+}
+
 // The infinite ones of two halves, 0 in place of the others.
 template <typename E>
 __device__ __forceinline__ unsigned infinite_halves(unsigned x)
@@ -138,7 +148,7 @@ __device__ __forceinline__ void merge_last(const PagedParams &p, float *lds, arr
             const float total = den == 0.f ? -INFINITY : M + (log2f(den) - Vec<E>::kLift);
             den_s[h] = den;
             if (p.lse) p.lse[row0 + h] = natural(total);
-            if (p.lse2) p.lse2[row0 + h] = total;
+            if (p.norm) p.norm[row0 + h] = norm_of<E>(at, den);
         }
     }
     __syncthreads();
@@ -454,7 +464,7 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
             if (ch == 0) {
                 const float total = den == 0.f ? -INFINITY : M + (log2f(den) - Vec<E>::kLift);
                 if (p.lse) p.lse[row0 + h] = natural(total);
-                if (p.lse2) p.lse2[row0 + h] = total;
+                if (p.norm) p.norm[row0 + h] = norm_of<E>(at, den);
             }
         } else {
             const size_t at_s = part * G + h;
@@ -481,12 +491,11 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(const PagedParams p)
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int h = 0; h < p.G; ++h) {
         const float4 s = *reinterpret_cast<const float4 *>(p.scores + (row0 + h) * p.n_pad + t);
-        const float total = p.lse2[row0 + h];
-        const float at = total > -INFINITY || total != total ? total : 0.f;       // nothing attended to: weights 0
-        sum.x += __builtin_amdgcn_exp2f(s.x - at);
-        sum.y += __builtin_amdgcn_exp2f(s.y - at);
-        sum.z += __builtin_amdgcn_exp2f(s.z - at);
-        sum.w += __builtin_amdgcn_exp2f(s.w - at);
+        const float2 n = p.norm[row0 + h];
+        sum.x = fmaf(__builtin_amdgcn_exp2f(s.x - n.x), n.y, sum.x);
+        sum.y = fmaf(__builtin_amdgcn_exp2f(s.y - n.x), n.y, sum.y);
+        sum.z = fmaf(__builtin_amdgcn_exp2f(s.z - n.x), n.y, sum.z);
+        sum.w = fmaf(__builtin_amdgcn_exp2f(s.w - n.x), n.y, sum.w);
     }
     const float *const in = p.w_in ? p.w_in + ((size_t)b * p.Hkv + g) * p.w_cap + t : nullptr;
     float *const out = p.w_out + ((size_t)b * p.Hkv + g) * p.w_cap + t;

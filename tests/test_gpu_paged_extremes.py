@@ -121,3 +121,22 @@ def test_infinite_values(dtype, D, B, N, splits, far):
             assert torch.equal(lse, clean[1])
             assert torch.equal(out.cpu()[kind == 0], clean[0].cpu()[kind == 0]), (at, b)
             c.v.copy_(was)
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("j", [4, 10, 16, 22, 24, 27, 30])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_weights_of_scores_of_every_size(dtype, sign, j, splits):
+    """The weights of a head add up to one however large its scores are."""
+    lens = [300, 37]
+    c, q, want = far_scores(j, sign, dtype, lens)
+    start = torch.rand(2, 2, 300, generator=c.g).cuda()
+    for w_in in (None, start):
+        w = torch.zeros(2, 2, 300, device="cuda")
+        attend(c, q, lens, splits=splits, scale=unit_scale(), weights=w, w_in=w_in, check=False)
+        for b, n in enumerate(lens):
+            p = 2 * want[b][0]                    # two query heads alike
+            total = p + (0 if w_in is None else w_in[b, :, :n].cpu().double())
+            # (at 2^30 the steps are 2^7, and 2^-128 is no normal number of fp32: what lies below 2^-126 may be 0)
+            ref.close(w[b, :, :n], total, p * rest(n, dtype) + 4 * 2.0 ** -23 * total + 2.0 ** -126, "weights")
