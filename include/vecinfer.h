@@ -530,7 +530,7 @@ size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q
  *   lse        fp32 [B, H_q] or NULL
  *   weights_in, weights_out  fp32 [B, H_kv, w_cap], w_cap >= N, or both NULL: for t < len_b
  *              weights_out[b, g, t] = weights_in[b, g, t] + sum over the G heads of softmax(s)_t
- *              (holes: + 0).  weights_in may be weights_out, or NULL: 0.  Rows t >= len_b are left as they
+ *              (holes and scores of -inf: + 0).  weights_in may be weights_out, or NULL: 0.  Rows t >= len_b are left as they
  *              were.  With weights a second launch follows.
  *   workspace  as for vecinfer_decode_attention
  * Errors: EINVAL (null or misaligned pointers, sizes, strides, scale (or scale log2 e) not finite, w_cap < N, weights_in alone),

@@ -492,10 +492,12 @@ __global__ __launch_bounds__(256) void paged_weights_kernel(const PagedParams p)
     for (int h = 0; h < p.G; ++h) {
         const float4 s = *reinterpret_cast<const float4 *>(p.scores + (row0 + h) * p.n_pad + t);
         const float2 n = p.norm[row0 + h];
-        sum.x = fmaf(__builtin_amdgcn_exp2f(s.x - n.x), n.y, sum.x);
-        sum.y = fmaf(__builtin_amdgcn_exp2f(s.y - n.x), n.y, sum.y);
-        sum.z = fmaf(__builtin_amdgcn_exp2f(s.z - n.x), n.y, sum.z);
-        sum.w = fmaf(__builtin_amdgcn_exp2f(s.w - n.x), n.y, sum.w);
+        // (a hole weighs 0, also where the head's sum is no number)
+        auto weight = [&](float score) { return score == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score - n.x) * n.y; };
+        sum.x += weight(s.x);
+        sum.y += weight(s.y);
+        sum.z += weight(s.z);
+        sum.w += weight(s.w);
     }
     const float *const in = p.w_in ? p.w_in + ((size_t)b * p.Hkv + g) * p.w_cap + t : nullptr;
     float *const out = p.w_out + ((size_t)b * p.Hkv + g) * p.w_cap + t;

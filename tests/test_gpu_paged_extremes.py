@@ -140,3 +140,22 @@ def test_weights_of_scores_of_every_size(dtype, sign, j, splits):
             total = p + (0 if w_in is None else w_in[b, :, :n].cpu().double())
             # (at 2^30 the steps are 2^7, and 2^-128 is no normal number of fp32: what lies below 2^-126 may be 0)
             ref.close(w[b, :, :n], total, p * rest(n, dtype) + 4 * 2.0 ** -23 * total + 2.0 ** -126, "weights")
+
+
+@pytest.mark.parametrize("splits", [1, 4])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_holes_weigh_nothing_beside_scores_that_are_no_numbers(splits, bad):
+    """A score that is no number leaves no number in the sums of the tokens that are there; a hole's stay as they were."""
+    c = Cache(1, 2, 64, 16, 160)
+    c.table[0, 2], c.table[0, 7] = -1, c.k.shape[0]
+    c.k[int(c.table[0, 4]), 1, 5, 6] = bad
+    q = c.queries(4).abs()
+    start = torch.rand(1, 2, 160, generator=c.g).cuda()
+    w = torch.zeros_like(start)
+    attend(c, q, splits=splits, weights=w, w_in=start, check=False)
+    hole = torch.zeros(160, dtype=torch.bool)
+    hole[32:48] = hole[112:128] = True
+    assert torch.equal(w[0, :, hole.cuda()], start[0, :, hole.cuda()])
+    assert torch.isnan(w[0, 1, 69]) and torch.isfinite(w[0, 0]).all()
+    if bad != bad:
+        assert torch.isnan(w[0, 1, ~hole.cuda()]).all()
