@@ -159,3 +159,37 @@ def test_holes_weigh_nothing_beside_scores_that_are_no_numbers(splits, bad):
     assert torch.isnan(w[0, 1, 69]) and torch.isfinite(w[0, 0]).all()
     if bad != bad:
         assert torch.isnan(w[0, 1, ~hole.cuda()]).all()
+
+
+@pytest.mark.parametrize("dtype", ref.DTYPES)
+@pytest.mark.parametrize("N,splits", [(150, 1), (150, 3), (4100, 0)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_what_is_read_in_place_of_a_hole(dtype, N, splits, weights):
+    """Infinities and NaN in the pages that are free, in page 0 (which is read in a hole's place) and behind the ends of sequences
+    with holes change nothing."""
+    c = Cache(3, 2, 128, 16, N, dtype, spare=40)
+    lens = [N - 80, N - 49, 0]
+    c.table[c.table == 0] = -1
+    c.table[0, 1] = -1
+    c.table[1, ::2] = c.k.shape[0] + 1
+    c.table[1, 1] = 2 ** 31 - 1
+    c.k[0], c.v[0] = 0.0, 0.0
+    q = c.queries(8)
+
+    def once(check):
+        w = torch.full((3, 2, N), 0.5, device="cuda") if weights else None
+        return attend(c, q, lens, splits=splits, weights=w, check=check)
+
+    clean = once(True)
+    used = set(c.table.flatten().tolist())
+    free = [i for i in range(c.k.shape[0]) if i not in used]
+    assert 0 in free
+    for x, bad in ((c.k, float("nan")), (c.v, float("inf")), (c.v, float("nan")), (c.k, float("-inf"))):
+        x[free] = bad
+        for b, n in enumerate(lens):
+            for col in range(c.table.shape[1]):
+                page = int(c.table[b, col])
+                if 0 <= page < c.k.shape[0]:
+                    x[page, :, max(0, n - 16 * col):] = bad
+        again = once(False)
+        assert all(torch.equal(a, b) for a, b in zip(again, clean) if a is not None)
