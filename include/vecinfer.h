@@ -558,7 +558,8 @@ int vecinfer_paged_attention(const vecinfer_pages *pages, const void *q, const i
  *   dst_lens     int32 [B], not seq_lens
  *   dst_weights  fp32 [B, H_kv, dst_w_cap], dst_w_cap >= keep, not weights, or NULL: the kept tokens' weights
  *   kept         int32 [B, H_kv, keep] or NULL: their old indices, in order (rows from dst_lens on are left)
- *   workspace    vecinfer_evict_workspace_bytes(H_kv, B, N, keep) bytes, 256-byte aligned
+ *   workspace    vecinfer_evict_workspace_bytes(H_kv, B, N, keep) bytes, 256-byte aligned; one for more sequences, tokens or
+ *                kept tokens serves fewer
  * Errors: EINVAL (null or misaligned pointers, sizes, pools that do not match, dst_lens = seq_lens,
  * dst_weights = weights), EUNSUPPORTED (pages, B or H_kv above 65535, N > 2^30), EWORKSPACE, ELAUNCH.
  */

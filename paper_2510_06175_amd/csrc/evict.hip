@@ -444,17 +444,20 @@ int evict_parts(long long rows, long long N)
     return (int)(parts < kMaxParts ? parts : kMaxParts);
 }
 
-size_t evict_hist_elems(long long rows, long long N)
+// Stretches that the workspace has room for.  More rows have fewer parts each, and fewer in all where these come in whole numbers
+// (56 rows of 40000 tokens 224, 32 rows 256), so not as many as evict_parts makes, but a bound that grows with both: a
+// workspace for more rows or longer ones serves fewer and shorter ones.
+static size_t evict_room(long long rows, long long N)
 {
-    const int parts = evict_parts(rows, N);
-    return parts == 1 ? 0 : 3 * (size_t)rows * parts * kHist;
+    if (N <= kHeld) return 0;
+    const long long most = (N + kPart - 1) / kPart, least = (N + kHeldPart - 1) / kHeldPart;
+    const long long filled = rows * least > num_cus() ? rows * least : num_cus(), cut = rows * (most < kMaxParts ? most : kMaxParts);
+    return (size_t)(filled < cut ? filled : cut);
 }
 
-size_t evict_state_elems(long long rows, long long N)
-{
-    const int parts = evict_parts(rows, N);
-    return parts == 1 ? 0 : 3 * (size_t)rows * parts;
-}
+size_t evict_hist_elems(long long rows, long long N) { return 3 * evict_room(rows, N) * kHist; }
+
+size_t evict_state_elems(long long rows, long long N) { return 3 * evict_room(rows, N); }
 
 int launch_evict(const EvictParams &p, hipStream_t stream)
 {

@@ -199,3 +199,19 @@ def test_steps_of_odd_tensors():
         vb._steps(x[:1].expand(3, 2, 16, 64), "x", True)
     with pytest.raises(ValueError):
         vb._steps(x.transpose(2, 3), "x", False)
+
+
+def test_an_eviction_workspace_serves_fewer():
+    """The size grows with the batch, the tokens and what is kept, across the length from which a row is shared by workgroups."""
+    size = vb.lib().vecinfer_evict_workspace_bytes
+    for Hkv in (1, 8, 24):
+        for N in (32767, 32768, 32769, 40000, 65536, 100003, 131072, 1 << 20, 1 << 22):
+            sizes = [size(Hkv, B, N, 2048) for B in range(1, 80)]
+            assert sizes == sorted(sizes)
+    for B in (1, 3, 4, 7, 32, 33, 64):
+        for keep in (1, 2048, 50000):
+            sizes = [size(8, B, N, keep) for N in (1, 2000, 32768, 32769, 36865, 40000, 49152, 49153, 100000, 262144, 262145, 1 << 20, 1 << 21)]
+            assert sizes == sorted(sizes)
+    for N in (1000, 40000):
+        sizes = [size(8, 3, N, keep) for keep in (1, 100, 999, 1000, 1001, 39999, 40000, 40001)]
+        assert sizes == sorted(sizes)
