@@ -28,3 +28,26 @@ def test_a_workspace_of_more_sequences(N, made, runs):
                 got.append((lens, kept))
             assert all(torch.equal(a, b) for a, b in zip(*got))
             assert (got[0][0] == keep).all()
+
+
+@pytest.mark.parametrize("N,lens", [(40000, [40000, 20000, 33000]), (70000, [70000, 69999, 4097]), (300000, [300000, 1, 0])])
+@pytest.mark.parametrize("how", ["spread", "ties"])
+def test_everything_stays(N, lens, how):
+    """Rows of as many tokens as may stay, or fewer, over several workgroups: each lists behind what those before it have."""
+    c = Cache(len(lens), 1, 64, 1024, N, seed=N)
+    evict(c, weights(c, N, how), N, 10, 200, lens=lens, dP=512)
+    evict(c, weights(c, N, how), N + 500, 0, 0, lens=lens, dP=1024)
+
+
+@pytest.mark.parametrize("holes", ["start", "end", "every other", "most", "all"])
+@pytest.mark.parametrize("how", ["spread", "ties", "zero"])
+@pytest.mark.parametrize("keep,first,recent", [(20500, 3000, 4000), (15000, 0, 0), (100, 20, 50)])
+def test_holes(holes, how, keep, first, recent):
+    """Holes in rows that workgroups share, so many that more may stay than are there, and fewer, which end among equal weights."""
+    N, P = 40000, 64
+    c = Cache(2, 2, 64, P, N, seed=keep)
+    cols = c.table.shape[1]
+    where = {"start": slice(0, cols // 3), "end": slice(cols // 2, cols), "every other": slice(1, cols, 2), "most": slice(5, cols - 3), "all": slice(0, cols)}[holes]
+    c.table[0, where] = -1
+    c.table[1, where] = c.k.shape[0] + 7
+    evict(c, weights(c, N, how), keep, first, recent, lens=[N, N - 4321])

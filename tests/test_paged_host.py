@@ -215,3 +215,16 @@ def test_an_eviction_workspace_serves_fewer():
     for N in (1000, 40000):
         sizes = [size(8, 3, N, keep) for keep in (1, 100, 999, 1000, 1001, 39999, 40000, 40001)]
         assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("weights", [0, 1])
+def test_an_attention_workspace_serves_smaller_batches(weights):
+    """What one made for a batch has to hold for fewer and shorter sequences is their size for one split, to which an automatic call
+    goes down."""
+    L, p = vb.lib(), pages()
+    shapes = [(B, N) for B in (1, 2, 3, 5, 8, 33, 64, 65) for N in (1, 31, 33, 256, 257, 3999, 4000, 100000)]
+    size = {(B, N, s): L.vecinfer_paged_workspace_bytes(C.byref(p), 32, B, N, s, weights) for B, N in shapes for s in (0, 1)}
+    for B, N in shapes:
+        for b, n in shapes:
+            if b <= B and n <= N:
+                assert 0 < size[b, n, 1] <= size[B, N, 0]
