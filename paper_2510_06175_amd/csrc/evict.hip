@@ -406,12 +406,13 @@ __global__ __launch_bounds__(kSelect) void evict_stage_kernel(const EvictParams 
     }
 }
 
+// from_place: the first place of this launch
 template <int D, bool STREAM>
-__global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p)
+__global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p, int from_place)
 {
     constexpr int kLanes = D / 8;                         // 16-byte pieces of a row
     const int t = threadIdx.x, piece = t % kLanes;
-    const int j = blockIdx.x * (256 / kLanes) + t / kLanes, g = blockIdx.y, b = blockIdx.z;
+    const int j = from_place + (int)blockIdx.x * (256 / kLanes) + t / kLanes, g = blockIdx.y, b = blockIdx.z;
     if (j >= p.dst_lens[b]) return;
     const size_t bg = (size_t)b * p.Hkv + g;
     const int i = p.ids[bg * (p.keep < p.N ? p.keep : p.N) + j];
@@ -478,8 +479,13 @@ int launch_evict(const EvictParams &p, hipStream_t stream)
     }
     const int rows = 256 / (p.D / 8);
     const int most = p.keep < p.N ? p.keep : p.N;
-    const dim3 grid((unsigned)((most + rows - 1) / rows), (unsigned)p.Hkv, (unsigned)p.B);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p); };
+    // (up to 2^22 workgroups along the places: 2^32 threads and more are not launched)
+    auto go = [&](auto kernel) {
+        for (int at = 0; at < most; at += rows << 22) {
+            const int left = most - at < rows << 22 ? most - at : rows << 22;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((left + rows - 1) / rows), (unsigned)p.Hkv, (unsigned)p.B), dim3(256), 0, stream, p, at);
+        }
+    };
     const bool streams = 8ll * p.D * most * p.Hkv * p.B >= kStreamBytes;
     if (p.D == 128)
         streams ? go(evict_move_kernel<128, true>) : go(evict_move_kernel<128, false>);

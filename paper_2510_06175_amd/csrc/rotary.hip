@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr int kMostTokens = 4;                            // of a workgroup
+constexpr unsigned kGridX = 1u << 22;                     // most workgroups of a grid's first axis: 2^32 threads and more are not launched
 
 __global__ void rotary_table_kernel(const double *freqs, double base, int scaling, double factor, double low, double high,
                                     double orig_len, int R, uint64_t *table)
@@ -75,7 +76,7 @@ __device__ __forceinline__ void turn_across(uint4 &one, uint4 &two, const float2
     two = __builtin_bit_cast(uint4, v);
 }
 
-// grid (tokens / TPW, head groups); TPW tokens per workgroup, 1 << tpw_shift
+// grid (tokens / TPW, head groups, kGridX of the former each); TPW tokens per workgroup, 1 << tpw_shift
 template <typename E, int D, bool APPEND, bool STREAM>
 __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, int tpw_shift)
 {
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, in
     __shared__ float2 cs_s[kMostTokens * (D / 2)];
     const int t = threadIdx.x, u = t % kUnits, row = t / kUnits;
     const int tpw = 1 << tpw_shift, half = p.R / 2;
-    const unsigned tok0 = blockIdx.x << tpw_shift, n_tok = (unsigned)p.B * (unsigned)p.T;
+    const unsigned tok0 = (blockIdx.z * kGridX + blockIdx.x) << tpw_shift, n_tok = (unsigned)p.B * (unsigned)p.T;
 
     for (int i = t; i < tpw * half; i += kBlock) {
         const int k = i / half, j = i - k * half;
@@ -214,7 +215,8 @@ void start(const RotaryParams &p, hipStream_t stream)
         const int passes = rows_taken(0) / kRows;
         gy = (unsigned)(passes < 65535 ? passes : 65535);
     }
-    const dim3 grid((unsigned)((n_tok + (1 << shift) - 1) >> shift), gy);
+    const unsigned groups = (unsigned)((n_tok + (1 << shift) - 1) >> shift);
+    const dim3 grid(groups < kGridX ? groups : kGridX, gy, (groups + kGridX - 1) / kGridX);
     if (4 * n_tok * heads * D >= kStreamBytes)
         hipLaunchKernelGGL((rotary_kernel<E, D, APPEND, true>), grid, dim3(kBlock), 0, stream, p, shift);
     else
