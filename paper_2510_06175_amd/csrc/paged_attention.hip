@@ -424,6 +424,8 @@ __global__ __launch_bounds__(NW * 64) void paged_attention_kernel(const int32_t 
         tiles(std::true_type{}, again);
     }
 
+    asm volatile("" : "+v"(seen));                        // (here, or the swap would wait for the partials' stores, which lie behind it in order)
+
     // ---- the wavefronts join
     l = rows_sum(l);
     float *const o_s = lds, *const m_s = lds + NW * KG * D, *const l_s = m_s + NW * KG;
