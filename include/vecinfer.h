@@ -441,7 +441,9 @@ typedef struct vecinfer_rotary_cfg {
 
 /*
  * Turns per position of the R / 2 pairs, as 64-bit fractions of a turn: table[i] = f_i / (2 pi) mod 1 in
- * units of 2^-64, so that the angle of any position is exact to 2^-32 turns.  Made once per configuration.
+ * units of 2^-64, cut from an fp64 number.  Its product with a position is exact modulo one turn, so that the
+ * angle at position p is within |p| (2^-50 f_i / (2 pi) + 2^-64) + 2^-26 turns of the formula's: the table's
+ * error, and fp32's rounding of what sine and cosine are taken of.  Made once per configuration.
  *   freqs  fp64 [R / 2] on the device: frequencies (radians per position) in place of the formula's, or NULL
  *   table  uint64 [R / 2] on the device, fully overwritten
  * Errors: EINVAL for null or misaligned (8 bytes) pointers or values outside the ranges above;
@@ -518,11 +520,13 @@ size_t vecinfer_paged_workspace_bytes(const vecinfer_pages *pages, int32_t num_q
 /*
  * Attention of one new token per sequence over its pages (the new token among them: append first):
  *   s_t = scale q . k_t  over t < len_b that are not in a hole;   o = softmax(s) v;   L = log sum_t exp(s_t)
- * per (b, query head h), KV head h / G, G = H_q / H_kv in 1 .. 16.  Products and sums in fp32, one rounding of
- * the output.  Without a token to attend to (or with scores of -inf alone) o = 0 and L = -inf.  What the rows
- * behind a sequence's end hold is of no account, infinities and NaN included.  An infinite value of an attended
- * token makes its channel of the output infinite, however little the token weighs (two of opposite signs, or a
- * NaN, make it NaN).  Sums are divided last: bf16 values have to stay below 2^96.
+ * per (b, query head h), KV head h / G, G = H_q / H_kv in 1 .. 16.  Products and sums in fp32, and one rounding of
+ * the output.  Probabilities meet the values as two parts of the pages' type, together within 2^-17 (bf16) or
+ * 2^-23 (fp16, and 2^-40 of the largest) of them.  Without a token to attend to (or with scores of -inf alone)
+ * o = 0 and L = -inf.  What the rows behind a sequence's end hold is of no account, infinities and NaN included.
+ * An infinite value of an attended token makes its channel of the output infinite, however little the token
+ * weighs (two of opposite signs, or a NaN, make it NaN).  Sums are divided last: bf16 values have to stay below
+ * 2^96.
  *   q          [B, H_q, D] by strides {b, h}             out  [B, H_q, D], contiguous, of the pages' type
  *   seq_lens   int32 [B] or NULL: N tokens each; clamped to [0, N]
  *   N          1 <= N <= max_pages page_size, N <= 2^30

@@ -123,8 +123,15 @@ __device__ __forceinline__ unsigned wave_upto(unsigned v)
 __device__ __forceinline__ float natural(float log2_units) { return log2_units * kLn2; }
 
 // 16 bytes of a row.  STREAM: what goes through once need not displace anything from the caches; taken by calls that move
-// 64 MB and more.  What a smaller one reads the kernel before it may have left in the Infinity Cache (gradients of 3 x 4099
-// tokens x 8 heads, 50 MB: 9.7 us, streaming 10.6; out of memory 13.5 and 11.2), and what it writes stays in reach of the next.
+// 64 MB and more.  A smaller one reads what the kernel before it has left in the Infinity Cache, and writes for the next, and
+// the three together are faster with the caches, where the call by itself, out of memory, is faster without (us, cached /
+// streaming; left out of memory, right between a copy that writes its input and one that reads its output, in sum):
+//              8 MB                      32 MB                     64 MB                     128 MB                    256 MB
+//   rotary     4.4 / 4.0    9.8 / 9.9    9.1 / 9.3   21.7 / 22.9   15.4 / 14.9  39.4 / 38.9  26.9 / 24.4  71.9 / 70.9  50.3 / 46.0  160 / 135
+//   append     6.1 / 5.9   11.5 / 11.2  11.4 / 10.0  21.5 / 22.6   17.4 / 15.8  34.1 / 36.1  29.8 / 27.4  60.3 / 61.9
+//   eviction  12.0 / 10.8  18.8 / 19.1  20.4 / 18.4  35.4 / 37.3   31.5 / 28.4  57.6 / 60.7  54.1 / 48.7  99.8 / 106   80.7 / 75.5  191 / 178
+// 64 MB is where the sum of both columns turns for the rotary kernel; by the right one alone it would be 128 to 192 MB, by the
+// left one alone nothing.
 constexpr long long kStreamBytes = 64ll << 20;
 
 typedef unsigned words4 __attribute__((ext_vector_type(4)));

@@ -140,19 +140,19 @@ struct Cut {
 
 constexpr int32_t kDealt = 64;           // most sequences of a batch that is dealt by length: a lane each
 
-// A compute unit holds one workgroup (8 wavefronts of 150 registers), and two rounds of them are slower than one where all
-// are alike: a workgroup's start and end take 7 us (one sequence of 196608 tokens, 8 KV heads: 126 us in 32 splits, 141 in
-// 48, 136 in 64).  So as many as fill the chip once, and
+// A compute unit holds one workgroup (8 wavefronts of 170 registers), and two rounds of them are slower than one where all
+// are alike: a workgroup's start and end take 7 us (one sequence of 196608 tokens, 8 KV heads: 123 us in 32 splits, 136 in
+// 48, 128 in 64).  So as many as fill the chip once, and
 //   - no shorter than 64 tokens, two tiles, or 128 with more than eight query heads per KV head, whose merge is longer (one
-//     sequence, 4 / 1 heads, 500 tokens: 7.2 us in 4, 6.6 in 8, 6.8 in 16; 1000: 7.3 in 8, 6.8 in 16, 7.2 in 32; 8 / 1, 1000:
-//     7.8 in 8, 7.3 in 16, 8.5 in 32; 16 / 1, 2000: 10.7 in 16, 11.2 in 32);
-//   - whole up to 256 tokens, one round of a workgroup's wavefronts (200 tokens 5.6 us whole, 6.5 to 7.0 in splits);
+//     sequence, 4 / 1 heads, 500 tokens: 6.7 us in 4, 6.4 in 8, 6.2 in 16; 1000: 6.7 in 8, 6.6 in 16 and in 32; 8 / 1, 1000:
+//     7.1 in 8 and in 16, 7.8 in 32; 16 / 1, 2000: 9.9 in 16, 10.9 in 32);
+//   - whole up to 256 tokens, one round of a workgroup's wavefronts (200 tokens 5.7 us whole, 6.4 to 6.7 in splits);
 //   - more where one round would leave an eighth of the chip idle and splits are long (4000 tokens).
 // Sequences that come with lengths of their own, 4000 tokens and up, are dealt by length to one round of workgroups, or,
 // where there are more than a quarter as many as compute units per KV head, to so many rounds that each has one and there is
-// one round more (N / 8 to N tokens, in the same splits / dealt: 8 KV heads, 4 x 30000 62.3 / 54.8 us, 8 x 8000 35.6 /
-// 32.4, 16 x 8000 60.0 / 56.7, 64 x 6000 162 / 159; 4 KV heads, 9 x 30000 69.0 / 58.5; 32 x 8192 102 to 112, depending on which
-// come first, / 104, and 32 of 8192 each 163 whole, 168 dealt.  Shorter ones not: 32 x 2000 31.7 / 35, 4 x 1000 7.8 / 8.3).
+// one round more (N / 8 to N tokens, in the same splits / dealt: 8 KV heads, 4 x 30000 62.0 / 53.5 us, 8 x 8000 35.1 /
+// 31.5, 16 x 8000 60.7 / 54.8, 64 x 6000 160 / 157; 4 KV heads, 9 x 30000 67.5 / 55.0; 32 x 8192 102 to 113, depending on which
+// come first, / 102, and 32 of 8192 each 161 whole, 167 dealt.  Shorter ones not: 32 x 2000 31.7 / 35, 4 x 1000 7.8 / 8.3).
 Cut even_cut(const vecinfer_pages *p, int32_t B, int64_t N, int64_t worth)
 {
     const int64_t groups = (int64_t)B * p->num_kv_heads;

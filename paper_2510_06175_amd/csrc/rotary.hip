@@ -1,9 +1,11 @@
 // Rotary positions, alone and on the way into the paged cache.
 //
 // A pair (x1, x2) of channels at position p becomes m (x1 c - x2 s, x1 s + x2 c), c and s the cosine and sine of p f_i.
-// The angle is held in turns as a 64-bit fixed-point fraction F_i = f_i / 2 pi: p F_i modulo 2^64 is the fraction of a
-// turn exactly as the table has it at every position (fp32 angles are off by a twentieth of a radian at 10^6), and its
-// upper 32 bits go through sincospi.  The pairs of a token are the same in all heads: a workgroup works the cosines and
+// The angle is held in turns as a 64-bit fixed-point fraction F_i = f_i / 2 pi, cut from an fp64 number: p F_i modulo 2^64 is
+// the fraction of a turn exactly for the table's word, so that all that grows with the position is that number's own error,
+// within 2^-50 of F_i per position (fp32 angles are off by a twentieth of a radian at 10^6).  Its upper 32 bits go through
+// sincospi as an fp32 number, which is within 2^-26 turns, and moves sine and cosine by 2^-23 at most, next to the
+// rows' own rounding of 2^-11 or 2^-8.  The pairs of a token are the same in all heads: a workgroup works the cosines and
 // sines of its tokens out once, into LDS, a thread each.
 //
 // A thread owns 16 channels of a row, 8 pairs: two 16-byte pieces, in the half layout those that belong together, R / 2
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(const RotaryParams p, in
 // (8192 tokens, 32 heads: 24.4 us with one token, 25.5 with four; 48 heads of an append: 30.0 with two, 30.8 with four, 38
 // with one; 8 heads 11.2 with four, 14.0 with one).  Where there are fewer tokens than would fill the chip, one, and a
 // token's heads are dealt to several workgroups.
-// Streaming (load16): 8192 tokens out of memory 25.5 us, 29.0 otherwise; 512 no difference.
+// Streaming: load16.
 template <typename E, int D, bool APPEND>
 void start(const RotaryParams &p, hipStream_t stream)
 {
